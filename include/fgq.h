@@ -109,7 +109,7 @@ int32_t fgq_abi_version(void);
  * kind of access and the byte or element offset of the first: 1
  * activations, 2 weight planes, 3 codes, 4 scale bytes, 5 group scales,
  * 6 offset terms, 7 partial maxima, 8 layer outputs, 9 split-K sums, 10
- * activation codes), and clears the counts.  For testing, not for
+ * activation codes, 11 key/value cache), and clears the counts.  For testing, not for
  * production: the normal library (libfgq.so) returns FGQ_ERR_UNSUPPORTED.
  * FGQ_ERR_NULL if count is NULL; FGQ_ERR_HIP on a runtime error.
  */
@@ -556,6 +556,148 @@ fgq_status fgq_group_sums(const uint8_t* q, int32_t bits, int64_t B,
                           int32_t pad_h, int32_t pad_w, int32_t G,
                           int64_t row0, int64_t nrows, int32_t* P,
                           void* stream);
+
+/*
+ * Attention blocks at 8 and 4 bits (not part of the paper's method: the same
+ * integer arithmetic for the layers around its subject in language models).
+ * int8 products with one scale a token and one a channel, a key/value cache
+ * quantized in groups of channels as it is written, attention over it.
+ *
+ * Types of the calls' floating-point tensors.  An empty batch (M, T, B or
+ * max_q zero) is FGQ_OK and launches nothing.
+ */
+enum { FGQ_F32 = 0, FGQ_F16 = 1, FGQ_BF16 = 2 };
+
+/*
+ * fgq_quantize_rows -- each row of x to int8 with one scale: a = max_k |x[m][k]|,
+ * scale[m] = a / 127, q[m][k] = rint(x[m][k] * (127 / a)) (fp32, ties to
+ * even).  Rows of activations (a scale a token) and rows of weights (a scale
+ * an output channel) alike.  A row with a < 2^-120 gives zeros and scale 1; a
+ * row with a NaN or infinity gives zeros and scale NaN.
+ *
+ * x     [in]  M rows of K elements of type x_type, ldx >= K elements apart
+ * q     [out] M rows of ldq bytes, 16-byte aligned, ldq a multiple of 16 and
+ *             at least K rounded up to 128; bytes K up to that are set to
+ *             zero, later ones untouched
+ * scale [out] fp32 [M]
+ */
+fgq_status fgq_quantize_rows(const void* x, int32_t x_type, int64_t M,
+                             int64_t K, int64_t ldx, int8_t* q, int64_t ldq,
+                             float* scale, void* stream);
+
+/*
+ * fgq_gemm_i8 -- y[m][o] = (sum_k q[m][k] w[o][k]) * sx[m] * sw[o] + bias[o]:
+ * exact int32 sums, the scales multiplied one after the other and the bias
+ * added in fp32, one rounding to y's type.
+ *
+ * q, w    [in]  int8 rows as fgq_quantize_rows writes them: 16-byte aligned,
+ *               ldq / ldw bytes apart (multiples of 16, at least K rounded up
+ *               to 128), zeros from K up to that multiple of 128
+ * sx, sw  [in]  fp32 [M], [O]
+ * bias    [in]  fp32 [O] or NULL
+ * y       [out] M rows of O elements of type y_type, ldy >= O apart
+ * FGQ_ERR_UNSUPPORTED for K > 131071 (int32 sums).
+ *
+ * fgq_linear_i8 -- the same on floating-point rows: y = fgq_gemm_i8 of
+ * fgq_quantize_rows(x), value for value.
+ *   ws  [tmp] device buffer of fgq_linear_i8_ws_bytes(M, K, O) bytes, 16-byte
+ *             aligned, not kept between calls
+ */
+fgq_status fgq_gemm_i8(const int8_t* q, int64_t ldq, const float* sx, int64_t M,
+                       int64_t K, const int8_t* w, int64_t ldw, const float* sw,
+                       int64_t O, const float* bias, int32_t y_type, void* y,
+                       int64_t ldy, void* stream);
+size_t fgq_linear_i8_ws_bytes(int64_t M, int64_t K, int64_t O);
+fgq_status fgq_linear_i8(const void* x, int32_t x_type, int64_t ldx, int64_t M,
+                         int64_t K, const int8_t* w, int64_t ldw,
+                         const float* sw, int64_t O, const float* bias,
+                         int32_t y_type, void* y, int64_t ldy, void* ws,
+                         size_t ws_bytes, void* stream);
+
+/*
+ * A quantized, paged key/value cache.  A page holds P tokens (a power of two,
+ * 16 to 1024) of Hkv heads of D channels at `bits` (4 or 8) bits, in groups
+ * of G channels (32, 64 or 128, dividing D).  The cache is num_pages pages of
+ * fgq_kv_page_bytes bytes, 16-byte aligned.  In a page, each head in turn:
+ *   codes of the P keys     [P][D * bits / 8] bytes (4 bits: the even channel
+ *                           in the low nibble)
+ *   codes of the P values   likewise
+ *   parameters of the keys  uint32 [D / G][P]: bf16 lo in the low half, bf16
+ *                           step in the high half
+ *   parameters of the values likewise
+ * A code c stands for lo + step * c.  Writing a group x[0 .. G): lo = min x
+ * rounded down to bf16, step = (max x / 2 - lo / 2) * (2 / L) rounded up to
+ * bf16 (0 below 2^-120), L = 15 or 255, c = clamp(rint((x - lo) * (1 / step)),
+ * 0, L), all in fp32; so a value is at most half a step from what its code
+ * stands for (up to fp32 rounding).  A group with a NaN or infinity reads
+ * back NaN.  (fp32 values below the bf16 range count as infinite.)
+ *
+ * fgq_kv_page_bytes -- bytes of one page (0: invalid arguments).
+ *
+ * fgq_kv_write -- token t of k and v ([T][Hkv][D] of type `type`, strides in
+ * elements, channels contiguous) into slot slots[t] = page * P + place.
+ * Tokens with a slot outside [0, num_pages * P) are skipped.  Slots of one
+ * call must differ.
+ *
+ * fgq_kv_read -- the values of slots[t] into k and v, contiguous [T][Hkv][D]
+ * of type `type`; zeros for a slot outside the cache.
+ */
+size_t fgq_kv_page_bytes(int32_t Hkv, int32_t D, int32_t P, int32_t bits,
+                         int32_t G);
+fgq_status fgq_kv_write(const void* k, const void* v, int32_t type, int64_t T,
+                        int64_t k_stride_t, int64_t k_stride_h,
+                        int64_t v_stride_t, int64_t v_stride_h,
+                        const int64_t* slots, void* cache, int64_t num_pages,
+                        int32_t Hkv, int32_t D, int32_t P, int32_t bits,
+                        int32_t G, void* stream);
+fgq_status fgq_kv_read(const int64_t* slots, int64_t T, const void* cache,
+                       int64_t num_pages, int32_t Hkv, int32_t D, int32_t P,
+                       int32_t bits, int32_t G, int32_t type, void* k, void* v,
+                       void* stream);
+
+/*
+ * fgq_attn_kv -- softmax(scale * Q K^T) V over that cache, for B sequences of
+ * any lengths: sequence b has the query tokens [cu_q[b], cu_q[b + 1]) and the
+ * keys 0 .. kv_lens[b] - 1, key j in place j % P of page pages[b][j / P].
+ * Query heads h share key head h / (Hq / Hkv).  With causal, query i of the
+ * nq of a sequence stands at position kv_lens[b] - nq + i and sees the keys
+ * up to there, with window > 0 only the last `window` of them; without, it
+ * sees all keys.  A row that sees no key gives zeros (lse -infinity).
+ * Whatever the cache holds in places that a row does not see, NaN included,
+ * leaves that row alone.
+ *
+ * q      [in]  [T][Hq][D], type FGQ_F16 or FGQ_BF16, strides in elements,
+ *              channels contiguous
+ * cu_q   [in]  int32 [B + 1], not decreasing, within [0, T]
+ * max_q  [in]  at least the most queries of a sequence (later ones are not
+ *              computed)
+ * pages  [in]  int32 [B][max_pages]; entries beyond a sequence's keys are not
+ *              read, entries outside the cache read page 0 instead
+ * kv_lens [in] int32 [B], at most max_pages * P (more count as that)
+ * o      [out] [T][Hq][D] contiguous, q's type; tokens of no sequence are
+ *              not written
+ * lse    [out] fp32 [T][Hq], the natural logarithm of the rows' sums of
+ *              exponentials, or NULL
+ * ws     [tmp] fgq_attn_kv_ws_bytes(T, Hq, Hkv, D, B, max_q, max_pages * P)
+ *              bytes, 4-byte aligned, not kept between calls; may be NULL when
+ *              that is 0 (depends on the device's compute-unit count)
+ * The arithmetic: scores and softmax statistics in fp32, probabilities times
+ * the values' steps rounded to fp16, sums in fp32.  Results do not depend on
+ * the order of workgroups.
+ * FGQ_ERR_UNSUPPORTED for D other than 64, 128, 256, for type FGQ_F32 and for
+ * a window without causal.
+ */
+size_t fgq_attn_kv_ws_bytes(int64_t T, int32_t Hq, int32_t Hkv, int32_t D,
+                            int64_t B, int64_t max_q, int64_t max_keys);
+fgq_status fgq_attn_kv(const void* q, int32_t type, int64_t T, int32_t Hq,
+                       int64_t q_stride_t, int64_t q_stride_h,
+                       const int32_t* cu_q, int64_t B, int64_t max_q,
+                       const void* cache, int64_t num_pages, int32_t Hkv,
+                       int32_t D, int32_t P, int32_t bits, int32_t G,
+                       const int32_t* pages, int64_t max_pages,
+                       const int32_t* kv_lens, float scale, int32_t causal,
+                       int64_t window, void* o, float* lse, void* ws,
+                       size_t ws_bytes, void* stream);
 
 /*
  * Measurement utility (not part of the method): the rate of the int8 matrix

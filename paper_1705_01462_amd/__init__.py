@@ -39,6 +39,7 @@ _P = ctypes.c_void_p
 _I32 = ctypes.c_int32
 _I64 = ctypes.c_int64
 _SZ = ctypes.c_size_t
+_F32 = ctypes.c_float
 
 _SIGS = {
     "fgq_status_string": ([_I32], ctypes.c_char_p),
@@ -82,6 +83,17 @@ _SIGS = {
     "fgq_prepare_weights_w8": ([_P, _I64, _I64, _I32, _I32, _P, _SZ, _P], _I32),
     "fgq_conv2d_w8": ([_P, _I32, _P, _I64, _I64, _I64, _I64, _P, _I64, _I32, _I32, _I32, _I32,
                        _I32, _I32, _I32, _P, _P, _P], _I32),
+    "fgq_quantize_rows": ([_P, _I32, _I64, _I64, _I64, _P, _I64, _P, _P], _I32),
+    "fgq_gemm_i8": ([_P, _I64, _P, _I64, _I64, _P, _I64, _P, _I64, _P, _I32, _P, _I64, _P], _I32),
+    "fgq_linear_i8_ws_bytes": ([_I64, _I64, _I64], _SZ),
+    "fgq_linear_i8": ([_P, _I32, _I64, _I64, _I64, _P, _I64, _P, _I64, _P, _I32, _P, _I64, _P, _SZ, _P], _I32),
+    "fgq_kv_page_bytes": ([_I32, _I32, _I32, _I32, _I32], _SZ),
+    "fgq_kv_write": ([_P, _P, _I32, _I64, _I64, _I64, _I64, _I64, _P, _P, _I64, _I32, _I32, _I32, _I32, _I32, _P],
+                     _I32),
+    "fgq_kv_read": ([_P, _I64, _P, _I64, _I32, _I32, _I32, _I32, _I32, _I32, _P, _P, _P], _I32),
+    "fgq_attn_kv_ws_bytes": ([_I64, _I32, _I32, _I32, _I64, _I64, _I64], _SZ),
+    "fgq_attn_kv": ([_P, _I32, _I64, _I32, _I64, _I64, _P, _I64, _I64, _P, _I64, _I32, _I32, _I32, _I32, _I32, _P,
+                     _I64, _P, _F32, _I32, _I64, _P, _P, _P, _SZ, _P], _I32),
     "fgq_probe_mfma_i8": ([_I32, _I32, _P, _I64, _P], _I32),
 }
 
@@ -550,6 +562,220 @@ def fgq_group_sums(q, bits, shape, codes, O, R, S, stride, pad, G, row0, nrows, 
                               O, R, S, sh, sw, ph, pw, G, row0, nrows, _dev(P, torch.int32, "P"), _stream())
     _check(rc, "fgq_group_sums")
     return P
+
+
+# ---- attention blocks at 8 and 4 bits
+
+_TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}  # FGQ_F32, FGQ_F16, FGQ_BF16
+
+
+def _type(t, name):
+    code = _TYPES.get(t.dtype)
+    if code is None:
+        raise TypeError(f"{name} must be float32, float16 or bfloat16, got {t.dtype}")
+    return code
+
+
+def _rows(t, dtype, name):
+    """Pointer and row stride of a 2-d GPU tensor whose rows are contiguous."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch tensor")
+    if t.device.type != "cuda":
+        raise ValueError(f"{name} must be a GPU tensor")
+    if dtype is not None and t.dtype is not dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name} must be 2-d with contiguous rows")
+    # a single row may have any stride
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _size(t, n, name):
+    if t.numel() != n:
+        raise ValueError(f"{name} must hold {n} values, got {t.numel()}")
+
+
+def fgq_i8_row_bytes(K):
+    """Bytes of a quantized row: K rounded up to 128."""
+    return (K + 127) // 128 * 128
+
+
+def fgq_quantize_rows(x, q=None, scale=None):
+    """x: float32, float16 or bfloat16 [M][K] (rows may be strided).  Returns
+    (q int8 [M][fgq_i8_row_bytes(K)], zeros past K; scale fp32 [M])."""
+    px, ldx = _rows(x, None, "x")
+    M, K = x.shape
+    if q is None:
+        q = torch.empty((M, fgq_i8_row_bytes(K)), dtype=torch.int8, device=x.device)
+    if scale is None:
+        scale = torch.empty(M, dtype=torch.float32, device=x.device)
+    pq, ldq = _rows(q, torch.int8, "q")
+    if q.shape[0] != M or q.shape[1] < fgq_i8_row_bytes(K):
+        raise ValueError(f"q must be [{M}][at least {fgq_i8_row_bytes(K)}], got {tuple(q.shape)}")
+    _size(scale, M, "scale")
+    rc = lib().fgq_quantize_rows(px, _type(x, "x"), M, K, ldx, pq, ldq, _dev(scale, torch.float32, "scale"), _stream())
+    _check(rc, "fgq_quantize_rows")
+    return q, scale
+
+
+def _i8_weights(w, sw, K, bias):
+    pw, ldw = _rows(w, torch.int8, "w")
+    O = w.shape[0]
+    if w.shape[1] < (K + 127) // 128 * 128:
+        raise ValueError(f"w must have rows of at least {fgq_i8_row_bytes(K)} bytes (K = {K} rounded up to 128, "
+                         f"zeros past K), got {w.shape[1]}")
+    _size(sw, O, "sw")
+    if bias is not None:
+        _size(bias, O, "bias")
+    return (pw, ldw, O, _dev(sw, torch.float32, "sw"), None if bias is None else _dev(bias, torch.float32, "bias"))
+
+
+def _i8_out(y, M, O, dtype, device):
+    if y is None:
+        y = torch.empty((M, O), dtype=dtype, device=device)
+        return y, y.data_ptr(), O
+    py, ldy = _rows(y, dtype, "y")
+    if tuple(y.shape) != (M, O):
+        raise ValueError(f"y must be [{M}][{O}], got {tuple(y.shape)}")
+    return y, py, ldy
+
+
+def fgq_gemm_i8(q, sx, K, w, sw, bias=None, dtype=torch.float32, y=None):
+    """y[m][o] = (sum_k q[m][k] w[o][k]) sx[m] sw[o] + bias[o], of `dtype`.
+    q and w as fgq_quantize_rows returns them, K their row length."""
+    pq, ldq = _rows(q, torch.int8, "q")
+    M = q.shape[0]
+    if q.shape[1] < fgq_i8_row_bytes(K):
+        raise ValueError(f"q must have rows of at least {fgq_i8_row_bytes(K)} bytes, got {q.shape[1]}")
+    _size(sx, M, "sx")
+    pw, ldw, O, psw, pb = _i8_weights(w, sw, K, bias)
+    y, py, ldy = _i8_out(y, M, O, dtype, q.device)
+    rc = lib().fgq_gemm_i8(pq, ldq, _dev(sx, torch.float32, "sx"), M, K, pw, ldw, psw, O, pb, _type(y, "y"), py, ldy,
+                           _stream())
+    _check(rc, "fgq_gemm_i8")
+    return y
+
+
+def fgq_linear_i8_ws_bytes(M, K, O):
+    return int(lib().fgq_linear_i8_ws_bytes(M, K, O))
+
+
+def fgq_linear_i8(x, w, sw, bias=None, dtype=None, y=None, ws=None):
+    """The rows of x quantized to int8 (fgq_quantize_rows), times w (fgq_gemm_i8):
+    y [M][O] of `dtype` (default: x's)."""
+    px, ldx = _rows(x, None, "x")
+    M, K = x.shape
+    pw, ldw, O, psw, pb = _i8_weights(w, sw, K, bias)
+    y, py, ldy = _i8_out(y, M, O, dtype or x.dtype, x.device)
+    if ws is None:
+        ws = torch.empty(lib().fgq_linear_i8_ws_bytes(M, K, O), dtype=torch.uint8, device=x.device)
+    rc = lib().fgq_linear_i8(px, _type(x, "x"), ldx, M, K, pw, ldw, psw, O, pb, _type(y, "y"), py, ldy,
+                             _dev(ws, torch.uint8, "ws"), ws.numel(), _stream())
+    _check(rc, "fgq_linear_i8")
+    return y
+
+
+def fgq_kv_page_bytes(Hkv, D, P, bits, G):
+    return int(lib().fgq_kv_page_bytes(Hkv, D, P, bits, G))
+
+
+def fgq_kv_cache(num_pages, Hkv, D, P, bits, G, device="cuda"):
+    """Memory for a cache: uint8 [num_pages][Hkv][bytes of a head], not initialised."""
+    nb = fgq_kv_page_bytes(Hkv, D, P, bits, G)
+    if nb == 0:
+        raise ValueError(f"no such cache: Hkv={Hkv} D={D} P={P} bits={bits} G={G}")
+    return torch.empty((num_pages, Hkv, nb // Hkv), dtype=torch.uint8, device=device)
+
+
+def _cache(cache, D, P, bits, G):
+    """Pointer, pages and heads of a cache tensor."""
+    p = _dev(cache, torch.uint8, "cache")
+    if cache.dim() != 3:
+        raise ValueError("cache must be uint8 [pages][heads][bytes of a head]")
+    n, h, nb = cache.shape
+    if nb != 2 * P * (D * bits // 8 + (4 * (D // G) if G > 0 else 0)):
+        raise ValueError(f"cache has {nb} bytes a head and page, which does not fit D={D} P={P} bits={bits} G={G}")
+    return p, n, h
+
+
+def _heads(t, name):
+    """Pointer and strides of a [tokens][heads][channels] tensor with contiguous channels."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch tensor")
+    if t.device.type != "cuda":
+        raise ValueError(f"{name} must be a GPU tensor")
+    if t.dim() != 3 or t.stride(2) != 1:
+        raise ValueError(f"{name} must be [tokens][heads][channels] with contiguous channels")
+    return t.data_ptr(), t.stride(0), t.stride(1)
+
+
+def fgq_kv_write(k, v, slots, cache, P, bits, G):
+    """Tokens k, v [T][Hkv][D] into the cache at slots (int64 [T], page * P +
+    place; negative: skipped)."""
+    pk, kt, kh = _heads(k, "k")
+    pv, vt, vh = _heads(v, "v")
+    T, H, D = k.shape
+    pc, n, Hkv = _cache(cache, D, P, bits, G)
+    if v.shape != k.shape or v.dtype is not k.dtype or H != Hkv:
+        raise ValueError(f"k and v must both be [T][{Hkv}][D] of one type, got {tuple(k.shape)}, {tuple(v.shape)}")
+    _size(slots, T, "slots")
+    rc = lib().fgq_kv_write(pk, pv, _type(k, "k"), T, kt, kh, vt, vh, _dev(slots, torch.int64, "slots"), pc, n, Hkv, D,
+                            P, bits, G, _stream())
+    _check(rc, "fgq_kv_write")
+    return cache
+
+
+def fgq_kv_read(slots, cache, P, D, bits, G, dtype, k=None, v=None):
+    """The values of the cache's slots: (k, v), each [T][Hkv][D] of `dtype`."""
+    pc, n, Hkv = _cache(cache, D, P, bits, G)
+    T = slots.numel()
+    if k is None:
+        k = torch.empty((T, Hkv, D), dtype=dtype, device=cache.device)
+    if v is None:
+        v = torch.empty((T, Hkv, D), dtype=dtype, device=cache.device)
+    for t, name in ((k, "k"), (v, "v")):
+        _size(t, T * Hkv * D, name)
+    rc = lib().fgq_kv_read(_dev(slots, torch.int64, "slots"), T, pc, n, Hkv, D, P, bits, G, _type(k, "k"),
+                           _dev(k, dtype, "k"), _dev(v, dtype, "v"), _stream())
+    _check(rc, "fgq_kv_read")
+    return k, v
+
+
+def fgq_attn_kv_ws_bytes(T, Hq, Hkv, D, B, max_q, max_keys):
+    return int(lib().fgq_attn_kv_ws_bytes(T, Hq, Hkv, D, B, max_q, max_keys))
+
+
+def fgq_attn_kv(q, cu_q, max_q, cache, pages, kv_lens, P, bits, G, scale=None, causal=True, window=0, o=None,
+                lse=None, ws=None):
+    """Attention of the query tokens q [T][Hq][D] (float16 or bfloat16) over the
+    cache: cu_q int32 [B + 1] their sequences' bounds, max_q the most queries of
+    one, pages int32 [B][max_pages], kv_lens int32 [B].  scale defaults to
+    1 / sqrt(D).  Returns o [T][Hq][D]; lse (fp32 [T][Hq]) is filled if given."""
+    pq, qt, qh = _heads(q, "q")
+    T, Hq, D = q.shape
+    pc, n, Hkv = _cache(cache, D, P, bits, G)
+    if pages.dim() != 2 or cu_q.numel() != pages.shape[0] + 1 or kv_lens.numel() != pages.shape[0]:
+        raise ValueError("pages must be [B][max_pages], cu_q [B + 1], kv_lens [B]")
+    B, max_pages = pages.shape
+    if o is None:
+        o = torch.empty((T, Hq, D), dtype=q.dtype, device=q.device)
+    else:
+        _size(o, T * Hq * D, "o")
+    if lse is not None:
+        _size(lse, T * Hq, "lse")
+    if ws is None:
+        nb = lib().fgq_attn_kv_ws_bytes(T, Hq, Hkv, D, B, max_q, max_pages * P)
+        if nb:
+            ws = torch.empty(nb, dtype=torch.uint8, device=q.device)
+    rc = lib().fgq_attn_kv(pq, _type(q, "q"), T, Hq, qt, qh, _dev(cu_q, torch.int32, "cu_q"), B, max_q, pc, n, Hkv, D,
+                           P, bits, G, _dev(pages, torch.int32, "pages"), max_pages,
+                           _dev(kv_lens, torch.int32, "kv_lens"), D ** -0.5 if scale is None else scale,
+                           1 if causal else 0, window, _dev(o, q.dtype, "o"),
+                           None if lse is None else _dev(lse, torch.float32, "lse"),
+                           None if ws is None else _dev(ws, torch.uint8, "ws"), 0 if ws is None else ws.numel(),
+                           _stream())
+    _check(rc, "fgq_attn_kv")
+    return o
 
 
 def fgq_probe_mfma_i8(blocks, iters, out=None):

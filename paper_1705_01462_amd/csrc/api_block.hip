@@ -1,0 +1,177 @@
+// api_block.hip -- the extern "C" boundary of a quantized attention block's
+// operators (declared in include/fgq.h): host-side validation, then launch on
+// the caller's stream.
+#include <math.h>
+
+#include "i8gemm.h"
+#include "kvattn.h"
+
+using namespace fgq;
+
+namespace {
+
+bool aligned(const void* p, uintptr_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+
+fgq_status check_i8(int64_t M, int64_t K, int64_t O, int64_t ldw, int64_t ldy, int32_t y_type, const void* w) {
+  if (M < 0 || K < 1 || O < 1 || M >= (1LL << 31) || O >= (1LL << 31) || ldw < round_up(K, kI8RowStep) || ldw % 16 ||
+      ldy < O || !type_ok(y_type))
+    return FGQ_ERR_SHAPE;
+  if (K > kI8MaxK) return FGQ_ERR_UNSUPPORTED;
+  if (!aligned(w, 16)) return FGQ_ERR_SHAPE;
+  return FGQ_OK;
+}
+
+fgq_status check_cache(int64_t num_pages, int32_t Hkv, int32_t D, int32_t P, int32_t bits, int32_t G, KvGeom* c) {
+  if (bits != 4 && bits != 8) return FGQ_ERR_BITS;
+  if (num_pages < 1 || Hkv < 1 || D < 1 || P < 1 || num_pages >= (1LL << 31) || D > (1 << 16) || Hkv > (1 << 16))
+    return FGQ_ERR_SHAPE;
+  if ((G != 32 && G != 64 && G != 128) || D % G != 0) return FGQ_ERR_GROUP;
+  if (P < 16 || P > 1024 || (P & (P - 1)) != 0) return FGQ_ERR_UNSUPPORTED;
+  *c = KvGeom{num_pages, Hkv, D, P, bits, G};
+  return FGQ_OK;
+}
+
+bool kv_grid_ok(int64_t T, const KvGeom& c) { return T <= (1LL << 38) / (static_cast<int64_t>(c.Hkv) * c.D / 8); }
+
+}  // namespace
+
+extern "C" {
+
+fgq_status fgq_quantize_rows(const void* x, int32_t x_type, int64_t M, int64_t K, int64_t ldx, int8_t* q, int64_t ldq,
+                             float* scale, void* stream) {
+  if (M < 0 || K < 1 || ldx < K || !type_ok(x_type) || M >= (1LL << 31) || K >= (1LL << 31) ||
+      ldq < round_up(K, kI8RowStep) || ldq % 16)
+    return FGQ_ERR_SHAPE;
+  if (M == 0) return FGQ_OK;
+  if (!x || !q || !scale) return FGQ_ERR_NULL;
+  if (!aligned(q, 16) || !aligned(x, type_bytes(x_type))) return FGQ_ERR_SHAPE;
+  return launch_quantize_rows(x, x_type, M, K, ldx, q, ldq, scale, as_stream(stream));
+}
+
+fgq_status fgq_gemm_i8(const int8_t* q, int64_t ldq, const float* sx, int64_t M, int64_t K, const int8_t* w,
+                       int64_t ldw, const float* sw, int64_t O, const float* bias, int32_t y_type, void* y,
+                       int64_t ldy, void* stream) {
+  const fgq_status rc = check_i8(M, K, O, ldw, ldy, y_type, w);
+  if (rc != FGQ_OK) return rc;
+  if (ldq < round_up(K, kI8RowStep) || ldq % 16 || !aligned(q, 16)) return FGQ_ERR_SHAPE;
+  if (M == 0) return FGQ_OK;
+  if (!q || !sx || !w || !sw || !y) return FGQ_ERR_NULL;
+  const i8::I8Args a{q,   w,   sx,  sw, bias, y, ldq, ldw, ldy, static_cast<int32_t>(M), static_cast<int32_t>(O),
+                     static_cast<int32_t>(ceil_div(K, kI8RowStep))};
+  return launch_i8_few(a, y_type, as_stream(stream));
+}
+
+size_t fgq_linear_i8_ws_bytes(int64_t M, int64_t K, int64_t O) {
+  if (M < 1 || K < 1 || O < 1) return 0;
+  return static_cast<size_t>(M) * (round_up(K, kI8RowStep) + 4);
+}
+
+fgq_status fgq_linear_i8(const void* x, int32_t x_type, int64_t ldx, int64_t M, int64_t K, const int8_t* w,
+                         int64_t ldw, const float* sw, int64_t O, const float* bias, int32_t y_type, void* y,
+                         int64_t ldy, void* ws, size_t ws_bytes, void* stream) {
+  fgq_status rc = check_i8(M, K, O, ldw, ldy, y_type, w);
+  if (rc != FGQ_OK) return rc;
+  if (ldx < K || !type_ok(x_type) || !aligned(x, type_bytes(x_type))) return FGQ_ERR_SHAPE;
+  if (M == 0) return FGQ_OK;
+  if (!x || !w || !sw || !y) return FGQ_ERR_NULL;
+  if (!ws || !aligned(ws, 16) || ws_bytes < fgq_linear_i8_ws_bytes(M, K, O)) return FGQ_ERR_WORKSPACE;
+  const int64_t ldq = round_up(K, kI8RowStep);
+  int8_t* q = static_cast<int8_t*>(ws);
+  float* sx = reinterpret_cast<float*>(q + M * ldq);
+  rc = launch_quantize_rows(x, x_type, M, K, ldx, q, ldq, sx, as_stream(stream));
+  if (rc != FGQ_OK) return rc;
+  return fgq_gemm_i8(q, ldq, sx, M, K, w, ldw, sw, O, bias, y_type, y, ldy, stream);
+}
+
+size_t fgq_kv_page_bytes(int32_t Hkv, int32_t D, int32_t P, int32_t bits, int32_t G) {
+  KvGeom c;
+  return check_cache(1, Hkv, D, P, bits, G, &c) == FGQ_OK ? static_cast<size_t>(Hkv) * kv_head_bytes(P, D, bits, G) : 0;
+}
+
+fgq_status fgq_kv_write(const void* k, const void* v, int32_t type, int64_t T, int64_t k_stride_t, int64_t k_stride_h,
+                        int64_t v_stride_t, int64_t v_stride_h, const int64_t* slots, void* cache, int64_t num_pages,
+                        int32_t Hkv, int32_t D, int32_t P, int32_t bits, int32_t G, void* stream) {
+  KvGeom c;
+  const fgq_status rc = check_cache(num_pages, Hkv, D, P, bits, G, &c);
+  if (rc != FGQ_OK) return rc;
+  if (T < 0 || !type_ok(type) || !kv_grid_ok(T, c) || !aligned(k, type_bytes(type)) || !aligned(v, type_bytes(type)) ||
+      !aligned(cache, 16))
+    return FGQ_ERR_SHAPE;
+  if (T == 0) return FGQ_OK;
+  if (!k || !v || !slots || !cache) return FGQ_ERR_NULL;
+  return launch_kv_write(k, v, type, T, {k_stride_t, k_stride_h, v_stride_t, v_stride_h}, slots, c,
+                         static_cast<uint8_t*>(cache), as_stream(stream));
+}
+
+fgq_status fgq_kv_read(const int64_t* slots, int64_t T, const void* cache, int64_t num_pages, int32_t Hkv, int32_t D,
+                       int32_t P, int32_t bits, int32_t G, int32_t type, void* k, void* v, void* stream) {
+  KvGeom c;
+  const fgq_status rc = check_cache(num_pages, Hkv, D, P, bits, G, &c);
+  if (rc != FGQ_OK) return rc;
+  if (T < 0 || !type_ok(type) || !kv_grid_ok(T, c) || !aligned(k, type_bytes(type)) || !aligned(v, type_bytes(type)) ||
+      !aligned(cache, 16))
+    return FGQ_ERR_SHAPE;
+  if (T == 0) return FGQ_OK;
+  if (!k || !v || !slots || !cache) return FGQ_ERR_NULL;
+  return launch_kv_read(slots, T, c, static_cast<const uint8_t*>(cache), type, k, v, as_stream(stream));
+}
+
+size_t fgq_attn_kv_ws_bytes(int64_t T, int32_t Hq, int32_t Hkv, int32_t D, int64_t B, int64_t max_q,
+                            int64_t max_keys) {
+  if (T < 1 || B < 1 || max_q < 1 || max_keys < 1 || Hkv < 1 || Hq < Hkv || Hq % Hkv || D < 1) return 0;
+  return kv_attn_ws_bytes(T, Hq, Hkv, D, B, max_q, max_keys);
+}
+
+fgq_status fgq_attn_kv(const void* q, int32_t type, int64_t T, int32_t Hq, int64_t q_stride_t, int64_t q_stride_h,
+                       const int32_t* cu_q, int64_t B, int64_t max_q, const void* cache, int64_t num_pages,
+                       int32_t Hkv, int32_t D, int32_t P, int32_t bits, int32_t G, const int32_t* pages,
+                       int64_t max_pages, const int32_t* kv_lens, float scale, int32_t causal, int64_t window,
+                       void* o, float* lse, void* ws, size_t ws_bytes, void* stream) {
+  KvGeom c;
+  const fgq_status rc = check_cache(num_pages, Hkv, D, P, bits, G, &c);
+  if (rc != FGQ_OK) return rc;
+  if (D != 64 && D != 128 && D != 256) return FGQ_ERR_UNSUPPORTED;
+  if (window > 0 && !causal) return FGQ_ERR_UNSUPPORTED;
+  if (type != FGQ_F16 && type != FGQ_BF16) return type == FGQ_F32 ? FGQ_ERR_UNSUPPORTED : FGQ_ERR_SHAPE;
+  if (T < 0 || B < 0 || T >= (1LL << 31) || B >= (1LL << 31) || Hq < Hkv || Hq % Hkv != 0 || Hq > (1 << 16) ||
+      max_q < 0 || max_q > T || max_pages < 0 || max_pages * P > (1LL << 30) || window < 0 || !isfinite(scale) ||
+      !(scale > 0.0f) || !aligned(q, 2) || !aligned(o, 2) || !aligned(cache, 16))
+    return FGQ_ERR_SHAPE;
+  if (T == 0 || B == 0 || max_q == 0) return FGQ_OK;
+  if (!q || !cu_q || !cache || !kv_lens || !o || (max_pages > 0 && !pages)) return FGQ_ERR_NULL;
+  // workgroups are counted in 31 bits
+  if (static_cast<double>(B) * Hq * max_q * 2 >= 2147483648.0) return FGQ_ERR_UNSUPPORTED;
+  const size_t need = kv_attn_ws_bytes(T, Hq, Hkv, D, B, max_q, max_pages * P);
+  if (need && (!ws || !aligned(ws, 4) || ws_bytes < need)) return FGQ_ERR_WORKSPACE;
+  KvAttnArgs a{};
+  a.q = q;
+  a.q_st = q_stride_t;
+  a.q_sh = q_stride_h;
+  a.cu_q = cu_q;
+  a.cache = static_cast<const uint8_t*>(cache);
+  a.pages = pages;
+  a.kv_lens = kv_lens;
+  a.o = o;
+  a.lse = lse;
+  a.T = T;
+  a.page_bytes = Hkv * kv_head_bytes(P, D, bits, G);
+  a.max_pages = max_pages;
+  a.window = window;
+  a.B = static_cast<int32_t>(B);
+  a.Hq = Hq;
+  a.Hkv = Hkv;
+  a.D = D;
+  a.P = P;
+  a.pshift = __builtin_ctz(P);
+  a.num_pages = static_cast<int32_t>(num_pages);
+  a.G = G;
+  a.bits = bits;
+  a.type = type;
+  a.causal = causal ? 1 : 0;
+  a.max_q = static_cast<int32_t>(max_q);
+  a.ratio = Hq / Hkv;
+  a.scale_log2 = scale * 1.4426950408889634f;
+  return launch_kv_attn(a, ws, as_stream(stream));
+}
+
+}  // extern "C"

@@ -35,6 +35,7 @@ enum CheckSite : uint32_t {
   kSiteStoreY = 8,    // layer outputs (fp32 or codes)
   kSiteStorePart = 9, // split-K int32 sums
   kSiteStoreQ = 10,   // quantized activation codes
+  kSiteStoreCache = 11,  // codes and parameters of a key/value cache
 };
 
 #ifdef FGQ_CHECK

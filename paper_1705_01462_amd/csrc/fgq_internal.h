@@ -213,4 +213,12 @@ fgq_status launch_group_conv(const uint8_t* q, const float* sx,
                              const void* prepared, const ConvGeom& g, const LayerOut& out,
                              hipStream_t st);
 
+// Int8 rows with one scale a row (rowquant.hip): rows are padded with zeros
+// to a multiple of kI8RowStep bytes, and sums over k stay below 2^31 up to
+// kI8MaxK (128 * 128 * 131071, the codes of a caller's own weights included).
+constexpr int64_t kI8RowStep = 128;
+constexpr int64_t kI8MaxK = 131071;
+fgq_status launch_quantize_rows(const void* x, int32_t type, int64_t M, int64_t K, int64_t ldx, int8_t* q,
+                                int64_t ldq, float* scale, hipStream_t st);
+
 }  // namespace fgq

@@ -1,0 +1,39 @@
+// kvattn.h -- attention over the quantized, paged cache (kvcache.h): host-side
+// description of a call, shared by the dispatch (kvattn.hip) and the kernel's
+// instantiations (kvattn_d*.hip).
+#pragma once
+
+#include "elem.h"
+#include "kvcache.h"
+
+namespace fgq {
+
+struct KvAttnArgs {
+  const void* q;           // [T][Hq][D], strides in elements
+  int64_t q_st, q_sh;
+  const int32_t* cu_q;     // [B + 1]
+  const uint8_t* cache;
+  const int32_t* pages;    // [B][max_pages]
+  const int32_t* kv_lens;  // [B]
+  void* o;                 // [T][Hq][D]
+  float* lse;              // [T][Hq] or NULL
+  float* part;             // split sums: [T * Hq][splits][D + 2] (O, maximum, sum), or NULL
+  int64_t T, page_bytes, max_pages;
+  int64_t window;          // 0: none
+  int32_t B, Hq, Hkv, D, P, pshift, num_pages, G, bits, type, causal;
+  int32_t max_q, ratio;    // query heads a key head
+  float scale_log2;        // softmax scale * log2 e
+  int32_t tiles;           // row tiles a key head (of max_q queries)
+  int32_t splits, split_keys;
+};
+
+// One launch for a head size (kvattn_d*.hip); nt: 16-row blocks a wave;
+// share: the waves of a workgroup share one row tile and divide its keys.
+fgq_status launch_kv_attn_d64(const KvAttnArgs& a, int nt, bool share, hipStream_t st);
+fgq_status launch_kv_attn_d128(const KvAttnArgs& a, int nt, bool share, hipStream_t st);
+fgq_status launch_kv_attn_d256(const KvAttnArgs& a, int nt, bool share, hipStream_t st);
+
+size_t kv_attn_ws_bytes(int64_t T, int32_t Hq, int32_t Hkv, int32_t D, int64_t B, int64_t max_q, int64_t max_keys);
+fgq_status launch_kv_attn(KvAttnArgs a, void* ws, hipStream_t st);
+
+}  // namespace fgq

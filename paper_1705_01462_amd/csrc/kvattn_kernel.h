@@ -1,0 +1,637 @@
+// kvattn_kernel.h -- attention over the quantized cache.
+//
+// With key values lo + step * c in groups of G channels (c the code), a score is
+//   q . k = sum_g [ step_g (q_g . c_g) + lo_g sum(q_g) ],
+// and an output channel of group g is
+//   sum_j p_j (lo_jg + step_jg c_j) = sum_j (p_j step_jg) c_j + sum_j p_j lo_jg,
+// so both products run on the matrix cores with the codes themselves as one
+// operand and nothing is dequantized: keys' and values' steps and minima meet
+// scores and probabilities, which are D / (rows) times fewer.
+//
+// Codes become fp16 by one bit operation for two of them: a code in the low
+// bits of a half is the subnormal number c 2^-24 (the matrix cores take
+// subnormal operands as they are), one left in bits 4 to 7 is 16 c 2^-24.
+// There the query's channel is divided by 16 beforehand, and the output's
+// afterwards.
+//
+// The rows of a tile are the queries of the heads that share a key head
+// (row = query * ratio + head).  Scores are computed transposed, keys x rows:
+// a lane has row l % 16 and, of 16 keys, 4 (l / 16) + [0, 4) -- which is how the
+// probabilities have to stand as the second product's operand (the order of
+// the keys inside a sum is free), so nothing moves between lanes but the
+// rows' maxima.  The values' codes go to the same lanes: lane l has channels
+// l % 16 (G / 16) + [0, G / 16) of a group and the same keys, one short load a
+// key; two keys' codes are paired into the halves of a register.
+//
+// Running maxima are renewed only when a score passes the present one by
+// 2^kSlack (probabilities then reach 2^kSlack, which fp16 has room for), and
+// the values' steps are brought near 1 by a power of two per row and group,
+// renewed when a larger step comes (per row, so that a key that a row does not
+// see leaves it alone whatever its step is); both are rare, so the outputs' accumulators are
+// hardly ever rescaled.  Probabilities times steps are rounded to fp16 (11
+// bits, the range placed so that 2^-25 of the largest is still a normal
+// number); maxima, sums and accumulators are fp32.
+#pragma once
+
+#include <type_traits>
+
+#include "igemm.h"
+#include "kvattn.h"
+
+namespace fgq {
+namespace {
+
+typedef _Float16 kv8h __attribute__((ext_vector_type(8)));
+typedef float kv4f __attribute__((ext_vector_type(4)));
+
+constexpr float kSlack = 4.0f;     // log2 of how far a score may pass its row's maximum
+constexpr float kBoost = 2048.0f;  // 2^11: the largest rounded probability is 2^(4 + 11)
+constexpr int kAttnThreads = 256;
+constexpr int kAttnWaves = 4;
+
+__device__ inline kv8h frag(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  return __builtin_bit_cast(kv8h, ev4u{a, b, c, d});
+}
+
+// Eight codes as fp16 c 2^-24 (bits 8), or four c and four 16 c, times 2^-24
+// (bits 4): from w (and w2 with 8 bits).  Channel order: 4 bits 0 4 1 5 2 6 3 7.
+template <int kBits>
+__device__ inline kv8h key_frag(uint32_t w, uint32_t w2) {
+  if constexpr (kBits == 4) {
+    const uint32_t h = w >> 8;
+    return frag(w & 0x000F000Fu, w & 0x00F000F0u, h & 0x000F000Fu, h & 0x00F000F0u);
+  } else {
+    return frag(__builtin_amdgcn_perm(0, w, 0x0C010C00u), __builtin_amdgcn_perm(0, w, 0x0C030C02u),
+                __builtin_amdgcn_perm(0, w2, 0x0C010C00u), __builtin_amdgcn_perm(0, w2, 0x0C030C02u));
+  }
+}
+
+// The middle code.  Values' codes are taken relative to it, (c - mid) 2^-24,
+// by one packed subtraction for two: the matrix cores truncate what they add
+// to the magnitude of the running sum, and sums of c itself grow with the
+// number of keys where those of c - mid mostly cancel (uncentred, over 10^5
+// keys, the outputs' error was 2.8 times that of the fp32 form).
+template <int kBits>
+constexpr int kMidCode = kBits == 4 ? 8 : 128;
+
+// Codes of one channel of two keys as fp16, centred: n-th channel of a piece w
+// that has 16 bits of each key (4 bits: n < 4, 16 (c - mid) for odd n; 8 bits: n < 2).
+template <int kBits>
+__device__ inline uint32_t value_pair(uint32_t w, int n) {
+  typedef _Float16 v2h __attribute__((ext_vector_type(2)));
+  uint32_t c, mid;
+  if constexpr (kBits == 4) {
+    const uint32_t h = n < 2 ? w : w >> 8;
+    c = n % 2 ? h & 0x00F000F0u : h & 0x000F000Fu;
+    mid = n % 2 ? 0x80808080u : 0x80088008u;
+  } else {
+    c = n ? w >> 8 & 0x00FF00FFu : w & 0x00FF00FFu;
+    mid = 0x80808080u;
+  }
+  return __builtin_bit_cast(uint32_t, __builtin_bit_cast(v2h, c) + __builtin_bit_cast(v2h, mid));
+}
+
+// kNT: 16-row blocks a wave.  kShare: the four waves have the same rows and
+// divide the keys (and workgroups may too: splits); else each wave has rows of
+// its own and all the keys.  kKT: 16-key tiles a step (even).
+template <int kBits, int kD, int kG, int kNT, bool kShare, int kKT>
+struct KvAttn {
+  static constexpr int kNG = kD / kG;
+  static constexpr int kRow = kD * kBits / 8;          // bytes of a token
+  static constexpr int kGB = kG * kBits / 8;           // of one of its groups
+  static constexpr int kSteps = kG / 32;               // matrix steps of a group (32 channels)
+  static constexpr int kKW = kGB / 16;                 // words of a key's group a lane has
+  static constexpr int kVB = kGB / 16;                 // bytes of a value's group a lane has
+  static constexpr int kVP = kVB >= 2 ? kVB / 2 : 1;   // their 16-bit pieces (one byte: half a piece)
+  static constexpr int kCh = kG / 16;                  // channels of a group a lane has
+  static constexpr int kPer = kBits == 4 ? 4 : 2;      // channels a piece
+  static constexpr int kRows = 16 * kNT;
+  static constexpr int kKeys = 16 * kKT;
+  static constexpr int kPairs = kKT / 2;
+
+  struct Raw {
+    uint32_t k[kKT][kNG][kKW];
+    uint32_t v[kKT][4][kNG][kVB >= 4 ? kVB / 4 : 1];
+    ev4u kp[kKT][kNG], vp[kKT][kNG];
+  };
+
+  const KvAttnArgs& a;
+  int lane, c16, g;
+  const uint8_t* head;         // cache + this key head
+  const int32_t* pg;           // the sequence's pages
+  kv8h q[kNT][kNG][kSteps];
+  float qsum[kNT][kNG], rs[kNT];  // sums of the scaled queries * 2^-24, scores' factor
+  int lo[kNT], hi[kNT];        // visible keys of this lane's rows
+  kv4f acc[kNT][kD / 16];      // sums of rounded probabilities times centred codes
+  float losum[kNT][kNG], l[kNT], m[kNT];  // sums of p (lo + step mid), of p; running maxima
+  float lim[kNT][kNG], nrm[kNT][kNG];  // a power of two no visible step so far passed, kBoost / lim
+
+  __device__ explicit KvAttn(const KvAttnArgs& args) : a(args) {}
+
+  // ---- queries: scaled by a power of two so that fp16 holds them, in the keys' channel order
+  __device__ void load_q(int nt, int64_t at) {
+    float v[kNG][kSteps][8];
+    uint32_t big = 0;
+#pragma unroll
+    for (int gr = 0; gr < kNG; ++gr)
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s) {
+        const int64_t i = at + gr * kG + g * (kG / 4) + 8 * s;
+        if (a.type == FGQ_F16)
+          values8<FGQ_F16>(load8<FGQ_F16>(a.q, i), v[gr][s]);
+        else
+          values8<FGQ_BF16>(load8<FGQ_BF16>(a.q, i), v[gr][s]);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) big = max(big, __float_as_uint(v[gr][s][j]) & 0x7FFFFFFFu);
+      }
+    big = max(big, static_cast<uint32_t>(__shfl_xor(static_cast<int>(big), 16)));
+    big = max(big, static_cast<uint32_t>(__shfl_xor(static_cast<int>(big), 32)));
+    // 2^e times the row has its largest value in [2^13, 2^14); rows of zeros (and below 2^-100) keep e bounded
+    const int e = 140 - max(static_cast<int>(big >> 23), 27);
+    const float up = big >= 0x7F800000u ? __uint_as_float(0x7FC00000u) : ldexpf(1.0f, e);
+    rs[nt] = ldexpf(a.scale_log2, 24 - e);  // the codes' 2^-24 among it
+#pragma unroll
+    for (int gr = 0; gr < kNG; ++gr) {
+      float sum = 0.0f;
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s) {
+        kv8h f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int ch = kBits == 4 ? (j % 2) * 4 + j / 2 : j;
+          const bool high = kBits == 4 && ch % 2 == 1;
+          const _Float16 h = static_cast<_Float16>(v[gr][s][ch] * (high ? up * 0.0625f : up));
+          f[j] = h;
+          sum += high ? 16.0f * static_cast<float>(h) : static_cast<float>(h);
+        }
+        q[nt][gr][s] = f;
+      }
+      sum += __shfl_xor(sum, 16);
+      sum += __shfl_xor(sum, 32);
+      qsum[nt][gr] = sum * 0x1p-24f;
+    }
+  }
+
+  // ---- one step's bytes.  last: the largest key whose page is known to be the sequence's own
+  __device__ void load(Raw& r, int key0, int last) const {
+#pragma unroll
+    for (int t = 0; t < kKT; ++t) {
+      const int key = min(key0 + 16 * t, last & ~15);
+      const int pid = __builtin_amdgcn_readfirstlane(pg[key >> a.pshift]);
+      // a page number outside the cache reads page 0 instead of foreign memory
+      const int64_t page = static_cast<uint32_t>(pid) < static_cast<uint32_t>(a.num_pages) ? pid : 0;
+      const uint8_t* base = head + page * a.page_bytes;
+      const int at = key & (a.P - 1);
+      const uint8_t* kb = base + at * kRow;
+      const uint8_t* vb = base + (a.P + at) * kRow;
+      const uint8_t* kp = base + 2 * a.P * kRow + 4 * at;
+      const uint8_t* vp = kp + 4 * kNG * a.P;
+#pragma unroll
+      for (int gr = 0; gr < kNG; ++gr) {
+        const uint8_t* p = kb + c16 * kRow + gr * kGB + g * (4 * kKW);
+        if constexpr (kKW == 1) {
+          r.k[t][gr][0] = *reinterpret_cast<const uint32_t*>(p);
+        } else if constexpr (kKW == 2) {
+          const uint2 w = *reinterpret_cast<const uint2*>(p);
+          r.k[t][gr][0] = w.x;
+          r.k[t][gr][1] = w.y;
+        } else {
+#pragma unroll
+          for (int j = 0; j < kKW / 4; ++j) {
+            const ev4u w = reinterpret_cast<const ev4u*>(p)[j];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) r.k[t][gr][4 * j + e] = w[e];
+          }
+        }
+        r.kp[t][gr] = *reinterpret_cast<const ev4u*>(kp + 4 * gr * a.P + 16 * g);
+        r.vp[t][gr] = *reinterpret_cast<const ev4u*>(vp + 4 * gr * a.P + 16 * g);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint8_t* s = vb + (4 * g + i) * kRow + gr * kGB + c16 * kVB;
+          if constexpr (kVB == 1) {
+            r.v[t][i][gr][0] = *s;
+          } else if constexpr (kVB == 2) {
+            r.v[t][i][gr][0] = *reinterpret_cast<const uint16_t*>(s);
+          } else if constexpr (kVB == 4) {
+            r.v[t][i][gr][0] = *reinterpret_cast<const uint32_t*>(s);
+          } else {
+            const uint2 w = *reinterpret_cast<const uint2*>(s);
+            r.v[t][i][gr][0] = w.x;
+            r.v[t][i][gr][1] = w.y;
+          }
+        }
+      }
+    }
+  }
+
+  // ---- one step.  kMask: some row does not see some of its keys
+  template <bool kMask>
+  __device__ void compute(const Raw& r, int key0) {
+    // scores, keys x rows
+    kv4f S[kKT][kNT];
+#pragma unroll
+    for (int t = 0; t < kKT; ++t) {
+#pragma unroll
+      for (int gr = 0; gr < kNG; ++gr) {
+        kv4f d[kNT];
+#pragma unroll
+        for (int n = 0; n < kNT; ++n) d[n] = kv4f{0, 0, 0, 0};
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+          const kv8h kf = kBits == 4 ? key_frag<kBits>(r.k[t][gr][s], 0)
+                                     : key_frag<kBits>(r.k[t][gr][(2 * s) % kKW], r.k[t][gr][(2 * s + 1) % kKW]);
+#pragma unroll
+          for (int n = 0; n < kNT; ++n) d[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, q[n][gr][s], d[n], 0, 0, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float st = __uint_as_float(r.kp[t][gr][i] & 0xFFFF0000u), mn = bf16_f32(r.kp[t][gr][i]);
+#pragma unroll
+          for (int n = 0; n < kNT; ++n)
+            S[t][n][i] = gr == 0 ? fmaf(st, d[n][i], mn * qsum[n][gr])
+                                 : fmaf(st, d[n][i], fmaf(mn, qsum[n][gr], S[t][n][i]));
+        }
+      }
+    }
+    if constexpr (kMask) {
+#pragma unroll
+      for (int t = 0; t < kKT; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int key = key0 + 16 * t + 4 * g + i;
+#pragma unroll
+          for (int n = 0; n < kNT; ++n)
+            if (key < lo[n] || key >= hi[n]) S[t][n][i] = -INFINITY;
+        }
+    }
+    // running maxima
+    float top[kNT];
+    bool renew = false;
+#pragma unroll
+    for (int n = 0; n < kNT; ++n) {
+      float x = -INFINITY;
+#pragma unroll
+      for (int t = 0; t < kKT; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x = fmaxf(x, S[t][n][i]);
+      top[n] = x * rs[n];
+      renew |= top[n] > m[n] + kSlack;
+    }
+    if (__any(renew)) {
+#pragma unroll
+      for (int n = 0; n < kNT; ++n) {
+        float x = top[n];
+        x = fmaxf(x, __shfl_xor(x, 16));
+        x = fmaxf(x, __shfl_xor(x, 32));
+        const float mn = fmaxf(m[n], x);
+        const float f = mn == m[n] ? 1.0f : exp2f(m[n] - mn);
+        m[n] = mn;
+        l[n] *= f;
+#pragma unroll
+        for (int gr = 0; gr < kNG; ++gr) losum[n][gr] *= f;
+#pragma unroll
+        for (int j = 0; j < kD / 16; ++j) acc[n][j] *= f;
+      }
+    }
+    // largest steps
+    float st[kNT][kNG];
+    bool grow = false;
+#pragma unroll
+    for (int gr = 0; gr < kNG; ++gr)
+#pragma unroll
+      for (int n = 0; n < kNT; ++n) {
+        float x = 0.0f;
+#pragma unroll
+        for (int t = 0; t < kKT; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float s = __uint_as_float(r.vp[t][gr][i] & 0xFFFF0000u);
+            x = fmaxf(x, !kMask || S[t][n][i] != -INFINITY ? s : 0.0f);
+          }
+        st[n][gr] = x;
+        grow |= x > lim[n][gr];
+      }
+    if (__any(grow)) {
+#pragma unroll
+      for (int n = 0; n < kNT; ++n)
+#pragma unroll
+        for (int gr = 0; gr < kNG; ++gr) {
+          float x = st[n][gr];
+          x = fmaxf(x, __shfl_xor(x, 16));
+          x = fmaxf(x, __shfl_xor(x, 32));
+          // two powers of two above the next one: steps of later keys rarely pass it
+          const float nl = __uint_as_float(min((__float_as_uint(x) & 0x7F800000u) + (3u << 23), 254u << 23));
+          const float f = x > lim[n][gr] ? lim[n][gr] / nl : 1.0f;
+          lim[n][gr] = x > lim[n][gr] ? nl : lim[n][gr];
+          nrm[n][gr] = kBoost / lim[n][gr];
+#pragma unroll
+          for (int c = 0; c < kCh; ++c) acc[n][gr * kCh + c] *= f;
+        }
+    }
+    // probabilities, and their products with steps and minima
+    uint32_t p[kPairs][kNG][kNT][4];
+#pragma unroll
+    for (int t = 0; t < kKT; ++t) {
+      float pr[kNT][4];
+#pragma unroll
+      for (int n = 0; n < kNT; ++n) {
+        const float neg = m[n] == -INFINITY ? 0.0f : -m[n];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          pr[n][i] = __builtin_amdgcn_exp2f(fmaf(S[t][n][i], rs[n], neg));
+          l[n] += pr[n][i];
+        }
+      }
+#pragma unroll
+      for (int gr = 0; gr < kNG; ++gr) {
+        float vs[4], vl[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          vs[i] = __uint_as_float(r.vp[t][gr][i] & 0xFFFF0000u);
+          vl[i] = fmaf(vs[i], static_cast<float>(kMidCode<kBits>), bf16_f32(r.vp[t][gr][i]));
+        }
+#pragma unroll
+        for (int n = 0; n < kNT; ++n) {
+          float y[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            y[i] = pr[n][i] * nrm[n][gr] * vs[i];
+            float z = pr[n][i] * vl[i];
+            if constexpr (kMask) {  // a hidden key's parameters may be NaN
+              const bool see = S[t][n][i] != -INFINITY;
+              y[i] = see ? y[i] : 0.0f;
+              z = see ? z : 0.0f;
+            }
+            losum[n][gr] += z;
+          }
+          p[t / 2][gr][n][2 * (t % 2)] = pack_f16(y[0], y[1]);
+          p[t / 2][gr][n][2 * (t % 2) + 1] = pack_f16(y[2], y[3]);
+        }
+      }
+    }
+    // outputs
+#pragma unroll
+    for (int u = 0; u < kPairs; ++u)
+#pragma unroll
+      for (int gr = 0; gr < kNG; ++gr) {
+        kv8h pf[kNT];
+#pragma unroll
+        for (int n = 0; n < kNT; ++n) pf[n] = frag(p[u][gr][n][0], p[u][gr][n][1], p[u][gr][n][2], p[u][gr][n][3]);
+        uint32_t w[4][kVP];  // key pairs (0,1) (2,3) of both tiles
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+          const auto& x = r.v[2 * u + h / 2][2 * (h % 2)][gr];
+          const auto& y = r.v[2 * u + h / 2][2 * (h % 2) + 1][gr];
+          if constexpr (kVB <= 2) {
+            w[h][0] = x[0] | y[0] << 16;
+          } else {
+#pragma unroll
+            for (int j = 0; j < kVB / 4; ++j) {
+              w[h][2 * j] = __builtin_amdgcn_perm(y[j], x[j], 0x05040100u);
+              w[h][2 * j + 1] = __builtin_amdgcn_perm(y[j], x[j], 0x07060302u);
+            }
+          }
+        }
+#pragma unroll
+        for (int c = 0; c < kCh; ++c) {
+          const int pc = c / kPer, e = c % kPer;
+          const kv8h vf = frag(value_pair<kBits>(w[0][pc], e), value_pair<kBits>(w[1][pc], e),
+                               value_pair<kBits>(w[2][pc], e), value_pair<kBits>(w[3][pc], e));
+#pragma unroll
+          for (int n = 0; n < kNT; ++n)
+            acc[n][gr * kCh + c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pf[n], acc[n][gr * kCh + c], 0, 0, 0);
+        }
+      }
+  }
+
+  // ---- the lane's sums over its keys become the row's, the accumulators become values
+  __device__ void finish() {
+#pragma unroll
+    for (int n = 0; n < kNT; ++n) {
+      l[n] += __shfl_xor(l[n], 16);
+      l[n] += __shfl_xor(l[n], 32);
+#pragma unroll
+      for (int gr = 0; gr < kNG; ++gr) {
+        float z = losum[n][gr];
+        z += __shfl_xor(z, 16);
+        z += __shfl_xor(z, 32);
+#pragma unroll
+        for (int c = 0; c < kCh; ++c) {
+          const bool high = kBits == 4 && c % 2 == 1;
+          kv4f& x = acc[n][gr * kCh + c];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x[i] = fmaf(x[i] * ((high ? 0x1p20f : 0x1p24f) / kBoost), lim[n][gr], z);
+        }
+      }
+    }
+  }
+
+  __device__ void run() {
+    const int tid = threadIdx.x;
+    lane = tid % 64;
+    c16 = lane % 16;
+    g = lane / 16;
+    const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
+    // neighbouring workgroups of one sequence and head share its pages in an XCD's L2
+    int id = ig::xcd_swizzle(blockIdx.x, gridDim.x);
+    const int split = id % a.splits;
+    id /= a.splits;
+    const int tile = a.tiles - 1 - id % a.tiles;  // the longest (last rows of a causal head) first
+    id /= a.tiles;
+    const int h = id % a.Hkv, b = id / a.Hkv;
+    const int64_t q0 = max(0, min(a.cu_q[b], static_cast<int>(a.T)));
+    const int64_t q1 = max(q0, min(static_cast<int64_t>(a.cu_q[b + 1]), a.T));
+    const int nq = static_cast<int>(min(q1 - q0, static_cast<int64_t>(a.max_q)));
+    const int rows = nq * a.ratio;
+    const int row0 = (kShare ? tile : tile * kAttnWaves + wave) * kRows;
+    if (row0 >= rows) return;  // uniform over the wave; over the workgroup where waves meet (kShare)
+    const int n = static_cast<int>(max(int64_t{0}, min(static_cast<int64_t>(a.kv_lens[b]), a.max_pages * a.P)));
+    const int before = n - static_cast<int>(q1 - q0);  // keys before the first query's own
+    const int wmax = static_cast<int>(min(a.window, static_cast<int64_t>(1) << 30));
+    auto first_key = [&](int row) { return a.window ? max(0, before + row / a.ratio - wmax + 1) : 0; };
+    auto end_key = [&](int row) { return a.causal ? max(0, min(n, before + row / a.ratio + 1)) : n; };
+    head = a.cache + static_cast<int64_t>(h) * kv_head_bytes(a.P, kD, kBits, kG);
+    pg = a.pages + b * a.max_pages;
+    const int rl = min(row0 + kRows, rows) - 1;  // last row
+    // keys that some row sees, and keys that all rows see
+    int k0 = first_key(row0) & ~15, k1 = end_key(rl);
+    const int all0 = first_key(rl), all1 = end_key(row0);
+    if (a.splits > 1) {
+      k0 += split * a.split_keys;
+      k1 = min(k1, k0 + a.split_keys);
+    }
+#pragma unroll
+    for (int t = 0; t < kNT; ++t) {
+      const int row = min(row0 + 16 * t + c16, rl);
+      lo[t] = first_key(row);
+      hi[t] = min(end_key(row), k1);
+      load_q(t, (q0 + row / a.ratio) * a.q_st + (h * a.ratio + row % a.ratio) * a.q_sh);
+      m[t] = -INFINITY;
+      l[t] = 0.0f;
+#pragma unroll
+      for (int gr = 0; gr < kNG; ++gr) {
+        losum[t][gr] = 0.0f;
+        lim[t][gr] = 0x1p-100f;
+        nrm[t][gr] = kBoost * 0x1p100f;
+      }
+#pragma unroll
+      for (int j = 0; j < kD / 16; ++j) acc[t][j] = kv4f{0, 0, 0, 0};
+    }
+    const int first = k0 + (kShare ? wave * kKeys : 0), hop = kShare ? kAttnWaves * kKeys : kKeys;
+    const int last = k1 - 1;
+    Raw r;
+    for (int key = first; key < k1; key += hop) {
+      load(r, key, last);
+      if (key >= all0 && key + kKeys <= min(all1, k1))
+        compute<false>(r, key);
+      else
+        compute<true>(r, key);
+    }
+    finish();
+    if constexpr (kShare)
+      join(split, rows, row0, q0, h, wave);
+    else
+      store(rows, row0, q0, h);
+  }
+
+  __device__ int64_t out_row(int64_t q0, int h, int row) const {
+    return (q0 + row / a.ratio) * a.Hq + h * a.ratio + row % a.ratio;
+  }
+
+  __device__ void put(int64_t orow, int ch, const float* v, int count) const {
+    if (!check_store(kSiteStoreY, orow * kD + ch, count, a.T * a.Hq * kD)) return;
+    for (int j = 0; j < count; ++j) {
+      if (a.type == FGQ_F16)
+        Elem<FGQ_F16>::put(a.o, orow * kD + ch + j, v[j]);
+      else
+        Elem<FGQ_BF16>::put(a.o, orow * kD + ch + j, v[j]);
+    }
+  }
+
+  // log sum exp of a row (natural logarithm), -inf for one that saw nothing
+  __device__ void put_lse(int64_t orow, float mx, float sum) const {
+    if (a.lse && check_store(kSiteStoreY, orow, 1, a.T * a.Hq))
+      a.lse[orow] = sum > 0.0f ? (mx + log2f(sum)) * 0.6931471805599453f : (sum == 0.0f ? -INFINITY : sum);
+  }
+
+  // ---- every wave its own rows
+  __device__ void store(int rows, int row0, int64_t q0, int h) {
+#pragma unroll
+    for (int n = 0; n < kNT; ++n) {
+      const int row = row0 + 16 * n + c16;
+      if (row >= rows) continue;
+      const int64_t orow = out_row(q0, h, row);
+      const float inv = l[n] == 0.0f ? 0.0f : 1.0f / l[n];
+      if (g == 0) put_lse(orow, m[n], l[n]);
+#pragma unroll
+      for (int gr = 0; gr < kNG; ++gr)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float v[kCh];
+#pragma unroll
+          for (int c = 0; c < kCh; ++c) v[c] = l[n] == 0.0f ? 0.0f : acc[n][gr * kCh + c][i] * inv;
+          put(orow, gr * kG + (4 * g + i) * kCh, v, kCh);
+        }
+    }
+  }
+
+  // ---- the waves' parts of the same rows, 64 / kNT channels a round
+  __device__ void join(int split, int rows, int row0, int64_t q0, int h, int wave) {
+    constexpr int kTiles = 8 / kNT;                   // accumulator tiles a round
+    constexpr int kRounds = (kD / 16 + kTiles - 1) / kTiles;
+    __shared__ float sm[kAttnWaves][kRows], sl[kAttnWaves][kRows];
+    __shared__ float so[kAttnWaves][kTiles][kRows][16];
+    if (g == 0)
+#pragma unroll
+      for (int n = 0; n < kNT; ++n) {
+        sm[wave][16 * n + c16] = m[n];
+        sl[wave][16 * n + c16] = l[n];
+      }
+    __syncthreads();
+    float total[kNT], mx[kNT];
+#pragma unroll
+    for (int n = 0; n < kNT; ++n) {
+      mx[n] = -INFINITY;
+      for (int w = 0; w < kAttnWaves; ++w) mx[n] = fmaxf(mx[n], sm[w][16 * n + c16]);
+      const float base = mx[n] == -INFINITY ? 0.0f : mx[n];
+      total[n] = 0.0f;
+      for (int w = 0; w < kAttnWaves; ++w) total[n] += sl[w][16 * n + c16] * exp2f(sm[w][16 * n + c16] - base);
+      const float f = exp2f(m[n] - base);
+#pragma unroll
+      for (int j = 0; j < kD / 16; ++j) acc[n][j] *= f;
+    }
+    for (int n = 0; n < kNT; ++n) {
+      const int row = row0 + 16 * n + c16;
+      if (wave == 0 && g == 0 && row < rows) {
+        const int64_t orow = out_row(q0, h, row);
+        if (a.splits == 1) {
+          put_lse(orow, mx[n], total[n]);
+        } else if (check_store(kSiteStorePart, (orow * a.splits + split) * (kD + 2) + kD, 2,
+                               a.T * a.Hq * a.splits * (kD + 2))) {
+          a.part[(orow * a.splits + split) * (kD + 2) + kD] = mx[n];
+          a.part[(orow * a.splits + split) * (kD + 2) + kD + 1] = total[n];
+        }
+      }
+    }
+#pragma unroll
+    for (int rd = 0; rd < kRounds; ++rd) {
+#pragma unroll
+      for (int n = 0; n < kNT; ++n)
+#pragma unroll
+        for (int j = 0; j < kTiles; ++j)
+          if (rd * kTiles + j < kD / 16)
+            *reinterpret_cast<kv4f*>(&so[wave][j][16 * n + c16][4 * g]) = acc[n][(rd * kTiles + j) % (kD / 16)];
+      __syncthreads();
+      for (int e = threadIdx.x; e < kTiles * kRows * 16; e += kAttnThreads) {
+        const int i = e % 16, rr = e / 16 % kRows, j = e / 16 / kRows, ti = rd * kTiles + j;
+        const int row = row0 + rr;
+        if (ti >= kD / 16 || row >= rows) continue;
+        float v = 0.0f, sum = 0.0f;
+        float mm = -INFINITY;
+        for (int w = 0; w < kAttnWaves; ++w) mm = fmaxf(mm, sm[w][rr]);
+        const float base = mm == -INFINITY ? 0.0f : mm;
+        for (int w = 0; w < kAttnWaves; ++w) {
+          v += so[w][j][rr][i];
+          sum += sl[w][rr] * exp2f(sm[w][rr] - base);
+        }
+        const int ch = ti / kCh * kG + i * kCh + ti % kCh;
+        const int64_t orow = out_row(q0, h, row);
+        if (a.splits == 1) {
+          v = sum == 0.0f ? 0.0f : v / sum;
+          put(orow, ch, &v, 1);
+        } else if (check_store(kSiteStorePart, (orow * a.splits + split) * (kD + 2) + ch, 1,
+                               a.T * a.Hq * a.splits * (kD + 2))) {
+          a.part[(orow * a.splits + split) * (kD + 2) + ch] = v;
+        }
+      }
+      __syncthreads();
+    }
+  }
+};
+
+template <int kBits, int kD, int kG, int kNT, bool kShare, int kKT>
+__global__ __launch_bounds__(kAttnThreads) void kv_attn_kernel(KvAttnArgs a) {
+  KvAttn<kBits, kD, kG, kNT, kShare, kKT> k(a);
+  k.run();
+}
+
+template <int kBits, int kD, int kG>
+fgq_status launch_one(const KvAttnArgs& a, int nt, bool share, hipStream_t st) {
+  constexpr int kKT = 2;
+  const dim3 grid(static_cast<uint32_t>(static_cast<int64_t>(a.B) * a.Hkv * a.tiles * a.splits)), wg(kAttnThreads);
+  if (share && nt == 1)
+    hipLaunchKernelGGL((kv_attn_kernel<kBits, kD, kG, 1, true, kKT>), grid, wg, 0, st, a);
+  else if (share)
+    hipLaunchKernelGGL((kv_attn_kernel<kBits, kD, kG, 2, true, kKT>), grid, wg, 0, st, a);
+  else
+    hipLaunchKernelGGL((kv_attn_kernel<kBits, kD, kG, 2, false, kKT>), grid, wg, 0, st, a);
+  return last_launch();
+}
+
+template <int kD, int kG>
+fgq_status launch_bits(const KvAttnArgs& a, int nt, bool share, hipStream_t st) {
+  return a.bits == 4 ? launch_one<4, kD, kG>(a, nt, share, st) : launch_one<8, kD, kG>(a, nt, share, st);
+}
+
+}  // namespace
+}  // namespace fgq

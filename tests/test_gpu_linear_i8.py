@@ -1,0 +1,193 @@
+"""GPU: int8 products with token and channel scales (fgq_quantize_rows,
+fgq_gemm_i8, fgq_linear_i8) against the definition: codes and scales bit for
+bit, outputs within the roundings of the epilogue (sum to fp32, two scales, bias:
+at most 4 units of 2^-24 of the magnitude) and of the output's type."""
+import numpy as np
+import pytest
+import torch
+
+import block_ref as ref
+
+fgq = pytest.importorskip("paper_1705_01462_amd")
+
+pytestmark = [pytest.mark.gpu,
+              pytest.mark.skipif(not torch.cuda.is_available(), reason="needs a GPU")]
+
+
+def inputs(M, K, O, dtype, seed, bias=True):
+    r = np.random.default_rng(seed)
+    x = torch.from_numpy((r.standard_normal((M, K)) * np.exp(r.standard_normal((M, 1)))).astype(np.float32)).to(dtype)
+    w = (r.standard_normal((O, K)) / np.sqrt(K)).astype(np.float32)
+    b = r.standard_normal(O).astype(np.float32) if bias else None
+    return x, w, b
+
+
+def check(y, want, mag):
+    u, tiny = ref.ROUND[y.dtype]
+    got = y.double().cpu().numpy()
+    tol = 4 * 2.0 ** -24 * mag * (1 + u) + u * np.abs(want) + tiny
+    bad = np.abs(got - want) > tol
+    assert not bad.any(), f"{bad.sum()} values off, worst {np.max(np.abs(got - want) / tol):.2f} of the bound"
+
+
+@pytest.mark.parametrize("dtype", ref.DTYPES)
+@pytest.mark.parametrize("M,K", [(1, 1), (3, 7), (2, 64), (5, 128), (7, 129), (4, 1000), (33, 2047), (2, 20011)])
+def test_rows(M, K, dtype):
+    x, _, _ = inputs(M, K, 1, dtype, 100 * M + K)
+    q, s = fgq.fgq_quantize_rows(x.cuda())
+    qr, sr = ref.rows(x.float().numpy())
+    assert q.shape == (M, fgq.fgq_i8_row_bytes(K))
+    q = q.cpu().numpy()
+    assert np.array_equal(q[:, :K], qr) and not q[:, K:].any()
+    assert np.array_equal(s.cpu().numpy(), sr)
+
+
+@pytest.mark.parametrize("dtype", ref.DTYPES)
+def test_rows_strided_and_unaligned(dtype):
+    """Rows of a wider matrix starting at an odd element; codes into wider rows."""
+    x, _, _ = inputs(9, 403, 1, dtype, 5)
+    xs = x.cuda()[:, 1:302]
+    out = torch.full((9, 512), 77, dtype=torch.int8, device="cuda")
+    q, s = fgq.fgq_quantize_rows(xs, q=out)
+    qr, sr = ref.rows(x[:, 1:302].float().numpy())
+    q = q.cpu().numpy()
+    assert np.array_equal(q[:, :301], qr) and not q[:, 301:384].any() and (q[:, 384:] == 77).all()
+    assert np.array_equal(s.cpu().numpy(), sr)
+
+
+def test_rows_of_zeros_tiny_values_and_values_that_are_not_finite():
+    x = np.zeros((8, 300), np.float32)
+    x[1, 5] = 2.0 ** -121            # counts as zeros
+    x[2, 7] = -2.0 ** -120           # does not
+    x[3, 299] = np.nan
+    x[4, 0] = np.inf
+    x[5, 130] = -np.inf
+    x[6] = 3.4e38
+    x[7, :3] = [1.0, 0.5 / 127, 1.5 / 127]   # ties
+    q, s = fgq.fgq_quantize_rows(torch.from_numpy(x).cuda())
+    qr, sr = ref.rows(x)
+    assert np.array_equal(q.cpu().numpy()[:, :300], qr)
+    assert np.array_equal(s.cpu().numpy(), sr, equal_nan=True)
+
+
+SHAPES = [(1, 1, 1), (1, 128, 16), (1, 4096, 100), (2, 130, 17), (4, 1000, 33), (16, 256, 64), (17, 384, 48),
+          (31, 2047, 129), (64, 512, 256), (65, 640, 250), (100, 2048, 1000), (129, 129, 127), (200, 1152, 260),
+          (257, 257, 511), (515, 2047, 300), (1024, 1024, 1024)]
+
+
+@pytest.mark.parametrize("dtype", ref.DTYPES)
+@pytest.mark.parametrize("M,K,O", SHAPES)
+def test_linear(M, K, O, dtype):
+    x, w, b = inputs(M, K, O, dtype, M + K + O, bias=O % 2 == 1)
+    wq, sw = fgq.fgq_quantize_rows(torch.from_numpy(w).cuda())
+    bias = None if b is None else torch.from_numpy(b).cuda()
+    y = fgq.fgq_linear_i8(x.cuda(), wq, sw, bias=bias)
+    assert y.dtype is dtype
+    qx, sx = ref.rows(x.float().numpy())
+    qw, swr = ref.rows(w)
+    want, mag = ref.product(qx, sx, qw, swr, b)
+    check(y, want, mag)
+    # quantizing and multiplying in two calls gives the same values
+    q, s = fgq.fgq_quantize_rows(x.cuda())
+    y2 = fgq.fgq_gemm_i8(q, s, K, wq, sw, bias=bias, dtype=dtype)
+    assert torch.equal(y, y2)
+
+
+@pytest.mark.parametrize("M", [1, 3, 40, 300])
+def test_linear_strides(M):
+    """x and y as columns of wider matrices, y of another type."""
+    K, O = 333, 70
+    x, w, b = inputs(M, K + 5, O, torch.float16, M, bias=True)
+    wq, sw = fgq.fgq_quantize_rows(torch.from_numpy(w[:, :K].copy()).cuda())
+    out = torch.full((M, O + 9), 7.0, dtype=torch.float32, device="cuda")
+    y = fgq.fgq_linear_i8(x.cuda()[:, 3:K + 3], wq, sw, bias=torch.from_numpy(b).cuda(), dtype=torch.float32,
+                          y=out[:, 5:O + 5])
+    qx, sx = ref.rows(x[:, 3:K + 3].float().numpy())
+    qw, swr = ref.rows(w[:, :K])
+    check(y, *ref.product(qx, sx, qw, swr, b))
+    o = out.cpu().numpy()
+    assert (o[:, :5] == 7).all() and (o[:, O + 5:] == 7).all()
+
+
+@pytest.mark.parametrize("M", [1, 5, 80, 400])
+def test_sums_at_the_ends_of_the_range(M):
+    """All codes 127 or -128 at the longest rows: the sums come near 2^31."""
+    K, O = 131071, 3
+    w = torch.full((O, fgq.fgq_i8_row_bytes(K)), -128, dtype=torch.int8, device="cuda")
+    w[1] = 127
+    w[:, K:] = 0
+    q = w[:1].expand(M, -1).contiguous()
+    one = torch.ones(max(M, O), device="cuda")
+    y = fgq.fgq_gemm_i8(q, one[:M].contiguous(), K, w, one[:O].contiguous())
+    want = np.array([[128 * 128 * K, -128 * 127 * K, 128 * 128 * K]], np.float64)
+    assert np.array_equal(y.double().cpu().numpy(), np.repeat(want.astype(np.float32).astype(np.float64), M, 0))
+
+
+@pytest.mark.parametrize("M", [2, 30, 300])
+def test_rows_that_are_not_finite_leave_the_others_alone(M):
+    x, w, _ = inputs(M, 200, 40, torch.bfloat16, 3)
+    wq, sw = fgq.fgq_quantize_rows(torch.from_numpy(w).cuda())
+    clean = fgq.fgq_linear_i8(x.cuda(), wq, sw)
+    x[1, 17] = float("nan")
+    y = fgq.fgq_linear_i8(x.cuda(), wq, sw)
+    assert torch.isnan(y[1]).all()
+    keep = [i for i in range(M) if i != 1]
+    assert torch.equal(y[keep], clean[keep])
+
+
+def test_empty_batch_and_other_streams():
+    _, w, b = inputs(1, 256, 64, torch.bfloat16, 1)
+    wq, sw = fgq.fgq_quantize_rows(torch.from_numpy(w).cuda())
+    x = torch.empty((0, 256), dtype=torch.bfloat16, device="cuda")
+    assert fgq.fgq_linear_i8(x, wq, sw).shape == (0, 64)
+    assert fgq.fgq_quantize_rows(x)[0].shape == (0, 256)
+    x = inputs(33, 256, 64, torch.bfloat16, 2)[0].cuda()
+    want = fgq.fgq_linear_i8(x, wq, sw)
+    st = torch.cuda.Stream()
+    st.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(st):
+        got = fgq.fgq_linear_i8(x, wq, sw)
+    torch.cuda.current_stream().wait_stream(st)
+    assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("M", [1, 24, 300])
+def test_replay_from_a_graph(M):
+    x, w, _ = inputs(M, 1024, 96, torch.float16, 4)
+    wq, sw = fgq.fgq_quantize_rows(torch.from_numpy(w).cuda())
+    xs = x.cuda()
+    y = torch.empty((M, 96), dtype=torch.float16, device="cuda")
+    ws = torch.empty(fgq.fgq_linear_i8_ws_bytes(M, 1024, 96), dtype=torch.uint8, device="cuda")
+    fgq.fgq_linear_i8(xs, wq, sw, y=y, ws=ws)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        fgq.fgq_linear_i8(xs, wq, sw, y=y, ws=ws)
+    for k in range(3):
+        xs.copy_(inputs(M, 1024, 96, torch.float16, 50 + k)[0])
+        want = fgq.fgq_linear_i8(xs, wq, sw).clone()
+        y.zero_()
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, want), k
+
+
+def test_refusals():
+    x, w, b = inputs(4, 100, 8, torch.float32, 1)
+    wq, sw = fgq.fgq_quantize_rows(torch.from_numpy(w).cuda())
+    xd = x.cuda()
+    for call, err in [
+            (lambda: fgq.fgq_linear_i8(x, wq, sw), ValueError),                        # not on the GPU
+            (lambda: fgq.fgq_linear_i8(xd.double(), wq, sw), TypeError),
+            (lambda: fgq.fgq_linear_i8(xd.t(), wq, sw), ValueError),                   # columns
+            (lambda: fgq.fgq_linear_i8(xd, wq[:, :112], sw), ValueError),              # rows not padded
+            (lambda: fgq.fgq_linear_i8(xd, wq, sw[:7]), ValueError),
+            (lambda: fgq.fgq_linear_i8(xd, wq.float(), sw), TypeError),
+            (lambda: fgq.fgq_linear_i8(xd, wq, sw, bias=sw[:3]), ValueError),
+            (lambda: fgq.fgq_linear_i8(xd, wq, sw, y=torch.empty(4, 9, device="cuda")), ValueError),
+            (lambda: fgq.fgq_linear_i8(xd, wq, sw, ws=torch.empty(16, dtype=torch.uint8, device="cuda")),
+             fgq.FgqError),
+            (lambda: fgq.fgq_gemm_i8(wq, sw, 200, wq, sw), ValueError)]:
+        with pytest.raises(err):
+            call()
