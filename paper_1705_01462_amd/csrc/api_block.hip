@@ -58,7 +58,7 @@ fgq_status fgq_gemm_i8(const int8_t* q, int64_t ldq, const float* sx, int64_t M,
   if (!q || !sx || !w || !sw || !y) return FGQ_ERR_NULL;
   const i8::I8Args a{q,   w,   sx,  sw, bias, y, ldq, ldw, ldy, static_cast<int32_t>(M), static_cast<int32_t>(O),
                      static_cast<int32_t>(ceil_div(K, kI8RowStep))};
-  return launch_i8_few(a, y_type, as_stream(stream));
+  return launch_i8(a, y_type, as_stream(stream));
 }
 
 size_t fgq_linear_i8_ws_bytes(int64_t M, int64_t K, int64_t O) {
@@ -76,6 +76,11 @@ fgq_status fgq_linear_i8(const void* x, int32_t x_type, int64_t ldx, int64_t M, 
   if (!x || !w || !sw || !y) return FGQ_ERR_NULL;
   if (!ws || !aligned(ws, 16) || ws_bytes < fgq_linear_i8_ws_bytes(M, K, O)) return FGQ_ERR_WORKSPACE;
   const int64_t ldq = round_up(K, kI8RowStep);
+  if (M <= kI8FusedRows && M * (ldq + 16) <= kI8FusedBytes) {
+    const i8::I8Args a{nullptr, w, nullptr, sw, bias, y, 0, ldw, ldy, static_cast<int32_t>(M), static_cast<int32_t>(O),
+                       static_cast<int32_t>(ceil_div(K, kI8RowStep))};
+    return launch_i8_fused(x, x_type, ldx, K, a, y_type, as_stream(stream));
+  }
   int8_t* q = static_cast<int8_t*>(ws);
   float* sx = reinterpret_cast<float*>(q + M * ldq);
   rc = launch_quantize_rows(x, x_type, M, K, ldx, q, ldq, sx, as_stream(stream));

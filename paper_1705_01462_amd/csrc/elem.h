@@ -97,25 +97,27 @@ __device__ inline uint32_t pack_bf16(float a, float b) {
   return __builtin_bit_cast(uint32_t, v2b{static_cast<__bf16>(a), static_cast<__bf16>(b)});
 }
 
+// The packs that hold eight values (rounded to the type).
+template <int kType>
+__device__ inline Raw8<kType> raw8(const float (&v)[8]) {
+  Raw8<kType> r;
+#pragma unroll
+  for (int e = 0; e < 4 * Raw8<kType>::kN; ++e) {
+    if constexpr (kType == FGQ_F32)
+      r.w[e / 4][e % 4] = __float_as_uint(v[e]);
+    else
+      r.w[0][e] = kType == FGQ_F16 ? pack_f16(v[2 * e], v[2 * e + 1]) : pack_bf16(v[2 * e], v[2 * e + 1]);
+  }
+  return r;
+}
+
 template <int kType>
 __device__ inline void store8(void* p, int64_t i, const float (&v)[8]) {
   typedef typename Pack<Elem<kType>::kBytes>::type pk;
   pk* d = reinterpret_cast<pk*>(static_cast<char*>(p) + i * Elem<kType>::kBytes);
-  if constexpr (kType == FGQ_F32) {
+  const Raw8<kType> r = raw8<kType>(v);
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      pk w;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) w[e] = __float_as_uint(v[4 * j + e]);
-      d[j] = w;
-    }
-  } else {
-    pk w;
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      w[e] = kType == FGQ_F16 ? pack_f16(v[2 * e], v[2 * e + 1]) : pack_bf16(v[2 * e], v[2 * e + 1]);
-    d[0] = w;
-  }
+  for (int j = 0; j < Raw8<kType>::kN; ++j) d[j] = pk{r.w[j].x, r.w[j].y, r.w[j].z, r.w[j].w};
 }
 
 // fn(integral_constant<type>) for a type that was validated.

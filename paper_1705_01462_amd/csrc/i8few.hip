@@ -1,70 +1,250 @@
 // i8few.hip -- the int8 product at few rows: a workgroup takes 16 channels
-// and 16 kMB rows, its waves share the steps of k and meet in LDS.
+// and 16 kMB rows, its eight waves share the steps of k and meet in LDS.
 //
-// The weights are what such a product has to read, and each is read once: a
-// lane holds channel l % 16 and, of every 64 k, the 16 at 16 (l / 16), so a
-// wave-wide load takes 64 contiguous bytes of 16 rows and goes straight into a
-// fragment of the 16x16x64 matrix instruction.  The result has a row of y in
-// every lane's column: lane l holds row l % 16, channels 4 (l / 16) + [0, 4).
+// The weights are what such a product has to read.  A wave takes every eighth
+// 128-byte step of k, of 16 channels and of the rows, several steps in flight:
+// the bytes in flight, not the instructions, set the rate.  Eight lanes load a
+// row's 128 bytes, and the fragments of the 16x16x64 matrix instruction (lane
+// l: row l % 16, k 16 (l / 16) of 64) are made through LDS of the wave's own.
+// (Loaded straight into fragments, neighbouring lanes read different rows, and
+// such loads run at a quarter of the rate: 37 B/ns a unit where rows of 128
+// bytes reach 130.)  The result has a row of y in every lane's column: lane l
+// holds row l % 16, channels 4 (l / 16) + [0, 4).
+//
+// kFused: x is not yet quantized.  Every workgroup then does that itself, while
+// its first weights are on their way: the rows' maxima, then their codes into
+// LDS, at a pitch 16 bytes off the bank period.  That saves a launch and its
+// wait; it reads x once a workgroup, so it is for small x.
 #include "i8gemm.h"
+#include "rowquant.h"
 
 namespace fgq {
 namespace {
 
 using namespace i8;
 using ig::v4i;
-constexpr int kWaves = 4;
+constexpr int kWaves = 8;
+constexpr int kThreads = 64 * kWaves;
+// Steps in flight a wave (16 registers each for the weights, as many for every 16 rows).
+template <int kMB>
+constexpr int kAheadFor = kMB <= 2 ? 4 : 3;
 
-template <int kMB, int kType>
-__global__ __launch_bounds__(64 * kWaves) void i8_few_kernel(I8Args a) {
-  __shared__ __attribute__((aligned(16))) v4i red[kWaves][kMB * 64];
-  const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+// LDS offset of a 16-byte slot of a row, swizzled so that fragment reads (8 or
+// 16 consecutive rows) touch every bank once.
+__device__ inline int frag_off(int row, int slot) { return row * 128 + 16 * (slot ^ ((row & 7) ^ (row >> 3 & 1))); }
+
+// Lanes of a wave exchange data through LDS: the compiler keeps the accesses
+// in this order, and the hardware does for the accesses of one wave.
+__device__ inline void wave_fence() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
+
+template <int kMB, int kXType, int kType>
+__global__ __launch_bounds__(kThreads, 1) void i8_few_kernel(I8Args a, const void* x, int64_t ldx, int64_t K) {
+  constexpr bool kFused = kXType >= 0;
+  extern __shared__ __attribute__((aligned(16))) unsigned char dyn[];  // fused: codes of the rows
+  constexpr int kAhead = kAheadFor<kMB>;
+  constexpr int kXRows = kFused ? 0 : 16 * kMB;  // rows of x a wave stages
+  // a wave's stage, later its sums
+  __shared__ __attribute__((aligned(16))) unsigned char stage[kWaves][(16 + kXRows) * 128];
+  static_assert((16 + kXRows) * 128 >= kMB * 1024, "");
+  __shared__ uint32_t rmax[kWaves];
+  __shared__ float rscale[16];
+  const int tid = threadIdx.x, lane = tid % 64;
+  const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
   const int g = lane / 16;
   const int n_ot = (a.O + 15) / 16;
   const int o0 = 16 * (blockIdx.x % n_ot);
   const int64_t m0 = static_cast<int64_t>(16 * kMB) * (blockIdx.x / n_ot);
-  const int8_t* wp = a.w + min(static_cast<int64_t>(o0 + lane % 16), static_cast<int64_t>(a.O) - 1) * a.ldw + 16 * g;
-  const int8_t* qp[kMB];
+  const int rows = static_cast<int>(min(static_cast<int64_t>(16 * kMB), a.M - m0));
+  const int64_t pitch = 128LL * a.nk + 16;
+
+  // lane l loads slot l % 8 of row l / 8 (+ 8, + 16, ...)
+  const int lrow = lane / 8, lslot = lane % 8;
+  const int8_t* wp[2];
 #pragma unroll
-  for (int b = 0; b < kMB; ++b)
-    qp[b] = a.q + min(m0 + 16 * b + lane % 16, static_cast<int64_t>(a.M) - 1) * a.ldq + 16 * g;
+  for (int j = 0; j < 2; ++j)
+    wp[j] = a.w + min(static_cast<int64_t>(o0 + 8 * j + lrow), static_cast<int64_t>(a.O) - 1) * a.ldw + 16 * lslot;
+  const int nw = (a.nk - wave + kWaves - 1) / kWaves;  // this wave's steps: wave, wave + kWaves, ...
+  v4i rw[kAhead][2];
+  auto load_w = [&](int u, int i) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) rw[u][j] = *reinterpret_cast<const v4i*>(wp[j] + 128LL * (wave + kWaves * i));
+  };
+#pragma unroll
+  for (int u = 0; u < kAhead; ++u)
+    if (u < nw) load_w(u, u);
+
+  float scale = 0.0f;  // fused: of row l % 16
+  if constexpr (kFused) {
+    // kPer waves a row (all eight for one row), each lane with every 64 kPer-th
+    // eight of it, the first kKeep in registers
+    constexpr int kKeep = kXType == FGQ_F32 ? 4 : 8;
+    const int per = rows == 1 ? 8 : rows == 2 ? 4 : rows <= 4 ? 2 : 1;
+    const int packs = static_cast<int>((K + 7) / 8), padded = 16 * a.nk, hop = 64 * per;
+    for (int r = wave / per; r < 16; r += kWaves / per) {
+      if (per == 1 && r >= rows) break;  // with several waves a row all of them meet below
+      const bool have = r < rows;
+      const int64_t at = (m0 + (have ? r : 0)) * ldx;
+      const int p0 = (wave % per) * 64 + lane;
+      // whole eights; the last values of a row that has no whole number of them
+      // belong to the lane whose turn it would be
+      const int whole = static_cast<int>(K / 8);
+      float last[8];
+      const bool tail = whole < packs && whole % hop == p0;
+      if (tail)
+        for (int j = 0; j < 8; ++j) last[j] = 8 * whole + j < K ? Elem<kXType>::get(x, at + 8 * whole + j) : 0.0f;
+      Raw8<kXType> keep[kKeep];
+#pragma unroll
+      for (int j = 0; j < kKeep; ++j)
+        if (p0 + hop * j < whole) keep[j] = load8<kXType>(x, at + 8 * (p0 + hop * j));
+      uint32_t m = 0;
+      auto add = [&](const float (&v)[8]) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) m = max(m, abs_bits(v[j]));
+      };
+#pragma unroll
+      for (int j = 0; j < kKeep; ++j)
+        if (p0 + hop * j < whole) {
+          float v[8];
+          values8<kXType>(keep[j], v);
+          add(v);
+        }
+      for (int p = p0 + hop * kKeep; p < whole; p += hop) {
+        float v[8];
+        values8<kXType>(load8<kXType>(x, at + 8 * p), v);
+        add(v);
+      }
+      if (tail) add(last);
+      m = wave_max(m);
+      if (per > 1) {
+        if (lane == 0) rmax[wave] = m;
+        __syncthreads();
+        for (int w = wave / per * per; w < wave / per * per + per; ++w) m = max(m, rmax[w]);
+      }
+      if (!have) break;
+      const RowScale s = row_scale(m);
+      if (lane == 0) rscale[r] = s.scale;
+      auto put = [&](int p, const float (&v)[8]) {
+        *reinterpret_cast<uint64_t*>(dyn + r * pitch + 8 * p) = row_codes8(v, s);
+      };
+#pragma unroll
+      for (int j = 0; j < kKeep; ++j)
+        if (p0 + hop * j < whole) {
+          float v[8];
+          values8<kXType>(keep[j], v);
+          put(p0 + hop * j, v);
+        }
+      for (int p = p0 + hop * kKeep; p < whole; p += hop) {
+        float v[8];
+        values8<kXType>(load8<kXType>(x, at + 8 * p), v);
+        put(p, v);
+      }
+      if (tail) put(whole, last);
+      for (int p = packs + p0; p < padded; p += hop) *reinterpret_cast<uint64_t*>(dyn + r * pitch + 8 * p) = 0;
+      if (per > 1) break;
+    }
+    __syncthreads();
+    scale = rscale[min(lane % 16, rows - 1)];
+  }
+
+  const int8_t* qp[2 * kMB];
+#pragma unroll
+  for (int j = 0; j < 2 * kMB; ++j) qp[j] = a.q + (m0 + min(8 * j + lrow, rows - 1)) * a.ldq + 16 * lslot;
+  const unsigned char* lp = dyn + min(lane % 16, rows - 1) * pitch + 16 * g;
+  v4i rx[kAhead][2 * kMB];
+  auto load_x = [&](int u, int i) {
+    if constexpr (!kFused)
+#pragma unroll
+      for (int j = 0; j < 2 * kMB; ++j) rx[u][j] = *reinterpret_cast<const v4i*>(qp[j] + 128LL * (wave + kWaves * i));
+  };
   v4i acc[kMB];
 #pragma unroll
   for (int b = 0; b < kMB; ++b) acc[b] = v4i{0, 0, 0, 0};
-  for (int s = wave; s < 2 * a.nk; s += kWaves) {
-    const v4i wf = *reinterpret_cast<const v4i*>(wp + 64 * static_cast<int64_t>(s));
 #pragma unroll
-    for (int b = 0; b < kMB; ++b) {
-      const v4i xf = *reinterpret_cast<const v4i*>(qp[b] + 64 * static_cast<int64_t>(s));
-      acc[b] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wf, xf, acc[b], 0, 0, 0);
+  for (int u = 0; u < kAhead; ++u)
+    if (u < nw) load_x(u, u);
+  unsigned char* const mine = stage[wave];
+  for (int i0 = 0; i0 < nw; i0 += kAhead) {
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int i = i0 + u;
+      if (i < nw) {
+        // a wave's LDS accesses are in order: the last step's reads are ahead of these writes
+#pragma unroll
+        for (int j = 0; j < 2; ++j) *reinterpret_cast<v4i*>(mine + frag_off(8 * j + lrow, lslot)) = rw[u][j];
+        if constexpr (!kFused)
+#pragma unroll
+          for (int j = 0; j < 2 * kMB; ++j)
+            *reinterpret_cast<v4i*>(mine + 2048 + frag_off(8 * j + lrow, lslot)) = rx[u][j];
+        if (i + kAhead < nw) {
+          load_w(u, i + kAhead);
+          load_x(u, i + kAhead);
+        }
+        wave_fence();
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const v4i wf = *reinterpret_cast<const v4i*>(mine + frag_off(lane % 16, 4 * h + g));
+#pragma unroll
+          for (int b = 0; b < kMB; ++b) {
+            v4i xf;
+            if constexpr (kFused)
+              xf = *reinterpret_cast<const v4i*>(lp + 128LL * (wave + kWaves * i) + 64 * h);
+            else
+              xf = *reinterpret_cast<const v4i*>(mine + 2048 + frag_off(16 * b + lane % 16, 4 * h + g));
+            acc[b] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wf, xf, acc[b], 0, 0, 0);
+          }
+        }
+        wave_fence();
+      }
     }
   }
+
 #pragma unroll
-  for (int b = 0; b < kMB; ++b) red[wave][64 * b + lane] = acc[b];
+  for (int b = 0; b < kMB; ++b) reinterpret_cast<v4i*>(mine)[64 * b + lane] = acc[b];
   __syncthreads();
-  for (int b = wave; b < kMB; b += kWaves) {
-    v4i S = red[0][64 * b + lane];
+  if (wave < kMB) {
+    v4i S = reinterpret_cast<const v4i*>(stage[0])[64 * wave + lane];
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) S += red[w][64 * b + lane];
-    const int64_t m = m0 + 16 * b + lane % 16;
-    if (m >= a.M) continue;
-    const float sx = a.sx[m];
+    for (int w = 1; w < kWaves; ++w) S += reinterpret_cast<const v4i*>(stage[w])[64 * wave + lane];
+    const int64_t m = m0 + 16 * wave + lane % 16;
+    if (16 * wave + lane % 16 < rows) {
+      const float sx = kFused ? scale : a.sx[m];
 #pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      const int o = o0 + 4 * g + c;
-      if (o < a.O) put_y<kType>(a, m, o, scaled(S[c], sx, a.sw[o], a.bias ? a.bias[o] : 0.0f));
+      for (int c = 0; c < 4; ++c) {
+        const int o = o0 + 4 * g + c;
+        if (o < a.O) put_y<kType>(a, m, o, scaled(S[c], sx, a.sw[o], a.bias ? a.bias[o] : 0.0f));
+      }
     }
   }
+}
+
+template <int kMB, int kXType, int kType>
+fgq_status launch(const I8Args& a, const void* x, int64_t ldx, int64_t K, hipStream_t st) {
+  const int64_t wgs = ceil_div(a.O, 16) * ceil_div(a.M, 16 * kMB);
+  if (wgs >= (1LL << 31)) return FGQ_ERR_UNSUPPORTED;
+  const uint32_t dyn = kXType < 0 ? 0 : static_cast<uint32_t>(a.M * (128 * a.nk + 16));
+  hipLaunchKernelGGL((i8_few_kernel<kMB, kXType, kType>), dim3(static_cast<uint32_t>(wgs)), dim3(kThreads), dyn, st, a,
+                     x, ldx, K);
+  return last_launch();
 }
 
 }  // namespace
 
 fgq_status launch_i8_few(const I8Args& a, int32_t y_type, hipStream_t st) {
   return with_type(y_type, [&](auto t) {
-    constexpr int kMB = 4;
-    const dim3 grid(static_cast<uint32_t>(ceil_div(a.O, 16) * ceil_div(a.M, 16 * kMB)));
-    hipLaunchKernelGGL((i8_few_kernel<kMB, decltype(t)::value>), grid, dim3(64 * kWaves), 0, st, a);
-    return last_launch();
+    constexpr int kType = decltype(t)::value;
+    if (a.M <= 16) return launch<1, -1, kType>(a, nullptr, 0, 0, st);
+    if (a.M <= 32) return launch<2, -1, kType>(a, nullptr, 0, 0, st);
+    if (a.M <= 48) return launch<3, -1, kType>(a, nullptr, 0, 0, st);
+    return launch<4, -1, kType>(a, nullptr, 0, 0, st);
+  });
+}
+
+fgq_status launch_i8_fused(const void* x, int32_t x_type, int64_t ldx, int64_t K, const I8Args& a, int32_t y_type,
+                           hipStream_t st) {
+  return with_type(x_type, [&](auto xt) {
+    return with_type(y_type, [&](auto t) {
+      return launch<1, decltype(xt)::value, decltype(t)::value>(a, x, ldx, K, st);
+    });
   });
 }
 

@@ -35,9 +35,34 @@ __device__ inline void put_y(const I8Args& a, int64_t m, int64_t o, float v) {
   if (check_store(kSiteStoreY, m * a.ldy + o, 1, (a.M - 1) * a.ldy + a.O)) Elem<kType>::put(a.y, m * a.ldy + o, v);
 }
 
+// Eight consecutive channels of a row (those below O), as wide stores.
+template <int kType>
+__device__ inline void put8(const I8Args& a, int64_t m, int64_t o, const float (&v)[8]) {
+  const int64_t at = m * a.ldy + o;
+  if (o + 8 > a.O) {
+    for (int c = 0; o + c < a.O; ++c) put_y<kType>(a, m, o + c, v[c]);
+  } else if (check_store(kSiteStoreY, at, 8, (a.M - 1) * a.ldy + a.O)) {
+    store8<kType>(a.y, at, v);
+  }
+}
+
+// Tiles of the output, rows by channels (one number: both), times the groups
+// of waves that share its k (i8tile.hip).
+enum Tile { kTile64x4, kTile64x2, kTile64by128x2, kTile128x2, kTile128, kTile256 };
+
 }  // namespace i8
 
 // Launchers; arguments already validated.
+fgq_status launch_i8(const i8::I8Args& a, int32_t y_type, hipStream_t st);
+fgq_status launch_i8_tile(const i8::I8Args& a, i8::Tile tile, int32_t y_type, hipStream_t st);
 fgq_status launch_i8_few(const i8::I8Args& a, int32_t y_type, hipStream_t st);
+// The same on rows that are not yet quantized (a.q and a.sx unused), at most
+// 16 of them, whose codes fit in LDS.
+fgq_status launch_i8_fused(const void* x, int32_t x_type, int64_t ldx, int64_t K, const i8::I8Args& a, int32_t y_type,
+                           hipStream_t st);
+// Measured, us (fused, two launches): K 4096, O 4096, 1 row 8.0, 10.1; 4 rows 8.8,
+// 10.3; 8 rows 10.4, 10.7; 16 rows (K 2048) 8.1, 7.6; K 16384, O 8192, 1 row
+// 31.2, 34.8.
+constexpr int64_t kI8FusedRows = 8, kI8FusedBytes = 64 << 10;
 
 }  // namespace fgq

@@ -1,0 +1,34 @@
+// i8gemm.hip -- which kernel an int8 product takes.
+//
+// Measured, us a product (few: i8few.hip; then rows x channels of a tile, and
+// the groups of waves that share its k; weights from memory):
+//                       few   64x64/4  64x64/2  64x128/2  128x128/2  128x128  256x256
+//   M   64 K 9216 O 4096  17.2   24.7     26.1
+//   M  256 K 4096 O  256   7.8   10.3     10.5    14.3       19.6      22.8     48.8
+//   M  100 K 4096 O 4096  17.5   12.6     14.2    18.3       24.2      31.2     49.2
+//   M  515 K 2047 O 1000  18.1    7.8      7.5    10.0       13.2      14.4     28.8
+//   M  400 K 4096 O 4096  74.9   23.0     20.0    18.5       22.4      30.6     50.0
+//   M  700 K 4096 O 4096  86.5   34.0     30.1    33.4       24.1      29.9     52.3
+//   M 2048 K 4096 O 4096         92       70      70         53        45       51
+//   M 4096 K 4096 O 4096 476    171      132     130        101        86       73
+//   M 8192 K 4096 O 8192                                              333      314
+// So: the smallest tile whose workgroups are all resident at once, with groups
+// (they hide what one workgroup a unit leaves idle); past that the larger tiles,
+// by rounds: 256 x 256 is one workgroup a unit, a round of it takes 1.7 times
+// that of two 128 x 128.
+#include "i8gemm.h"
+
+namespace fgq {
+
+fgq_status launch_i8(const i8::I8Args& a, int32_t y_type, hipStream_t st) {
+  const int64_t cus = ig::device_cus();
+  auto tiles = [&](int64_t rows, int64_t channels) { return ceil_div(a.M, rows) * ceil_div(a.O, channels); };
+  if (a.M <= 64 || tiles(64, 16) <= cus) return launch_i8_few(a, y_type, st);
+  if (tiles(64, 64) <= cus) return launch_i8_tile(a, a.nk >= 24 ? i8::kTile64x4 : i8::kTile64x2, y_type, st);
+  if (tiles(64, 128) <= cus) return launch_i8_tile(a, i8::kTile64by128x2, y_type, st);
+  if (tiles(128, 128) <= cus) return launch_i8_tile(a, i8::kTile128x2, y_type, st);
+  const int64_t large = 17 * ceil_div(tiles(256, 256), cus), middle = 10 * ceil_div(tiles(128, 128), 2 * cus);
+  return launch_i8_tile(a, large <= middle ? i8::kTile256 : i8::kTile128, y_type, st);
+}
+
+}  // namespace fgq

@@ -1,0 +1,250 @@
+// i8tile.hip -- the int8 product at many rows: tiles of the output, both
+// operands through LDS.
+//
+// Waves in a grid of kWO x kWM share a tile, each computing kBO x kBM 32x32
+// blocks of it.  A step is 128 bytes of k of every row and channel.  Two LDS
+// stages and a set of registers are in flight: while step s is computed, s + 1
+// goes from registers to the other stage and s + 2 from memory to registers.
+// A step's one barrier stands before its last fragment's products, which
+// cover the next stage's first reads; the reads, writes and loads of a phase
+// are spread over its matrix instructions.  With kG > 1 that many groups of
+// waves take the steps in turn, each with stages of its own, and add their
+// sums at the end: where a unit has one workgroup, one group leaves it idle
+// between a barrier and the reads after it.
+//
+// What bounds it: LDS.  Per step of a 256 x 256 tile a unit's waves read 192 KB
+// of fragments and write 64 KB, 2048 clocks at 128 B a clock, as long as the
+// matrix instructions take (128 x 128 a wave would read less, but one wave a
+// SIMD overlapped worse: 1.93 instead of 2.2 POP/s).  8192 x 8192 x 8192:
+// 500 us, 2.2 POP/s; 8192 rows x 4096 x 8192: 314 us, 1.75 POP/s (a prologue
+// and an epilogue a tile of 32 steps).
+//
+// The 16-byte slots of a row are XOR-swizzled, so publishing and fragment
+// reads touch every bank once.  The weights are the instruction's first
+// operand, their rows permuted so that a lane ends up with a row of y and 16
+// consecutive channels (stored as 16-byte pieces; with the instruction's own
+// order, 8 bytes, a 256 x 256 tile's epilogue took 24 us instead of 14).
+// Workgroups of one XCD take four tiles of rows times neighbouring tiles of
+// channels, so operands are read from its L2.
+#include "i8gemm.h"
+
+namespace fgq {
+namespace {
+
+using namespace i8;
+using ig::v16i;
+using ig::v4i;
+constexpr int kGroupM = 4;
+
+// The order of a phase's instructions: kR fragment reads, and kX others (LDS
+// writes 0x200 or loads 0x20), spread over its kN matrix instructions.
+template <int kN, int kR, int kX, int kMaskX, int kI = 0>
+__device__ inline void interleave() {
+  if constexpr (kI < kN) {
+    constexpr int r = (kI + 1) * kR / kN - kI * kR / kN, x = (kI + 1) * kX / kN - kI * kX / kN;
+    if constexpr (r > 0) __builtin_amdgcn_sched_group_barrier(0x100, r, 0);
+    __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+    if constexpr (x > 0) __builtin_amdgcn_sched_group_barrier(kMaskX, x, 0);
+    interleave<kN, kR, kX, kMaskX, kI + 1>();
+  }
+}
+
+// Fragment row r of 32 reads weight row order(r), so that the 16 results of a
+// lane (fragment rows 8 e + 4 (l / 32) + c) are 16 consecutive channels.
+__device__ inline int order(int r) { return 16 * (r >> 2 & 1) + 4 * (r >> 3) + (r & 3); }
+// LDS offset of a 16-byte slot of a row, XOR-swizzled so that 8 consecutive
+// fragment rows cover 128 bytes of banks, and 16 of them 256.
+__device__ inline int q_off(int row, int slot) { return row * 128 + 16 * (slot ^ ((row & 7) ^ (row >> 3 & 1))); }
+__device__ inline int w_off(int row, int slot) {  // row = order(r): by r
+  return row * 128 + 16 * (slot ^ ((row >> 2 & 4 | row & 3) ^ (row >> 2 & 1)));
+}
+
+template <int kWO, int kWM, int kBO, int kBM, int kG, int kType>
+__global__ __launch_bounds__(64 * kWO * kWM * kG, 2) void i8_tile_kernel(I8Args a, int n_mt, int n_ot) {
+  constexpr int kThreads = 64 * kWO * kWM;
+  constexpr int kTO = 32 * kWO * kBO, kTM = 32 * kWM * kBM;     // channels and rows of a tile
+  constexpr int kPO = kTO * 8 / kThreads, kPM = kTM * 8 / kThreads;  // 16-byte pieces a thread
+  constexpr int kStage = (kTO + kTM) * 128;
+  __shared__ __attribute__((aligned(16))) unsigned char lds_all[kG * 2 * kStage];
+  const int grp = kG == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / kThreads);
+  const int tid = threadIdx.x % kThreads, lane = tid % 64, wave = tid / 64;
+  unsigned char* const lds = lds_all + grp * 2 * kStage;
+
+  const int id = ig::xcd_swizzle(blockIdx.x, gridDim.x);
+  const int gm0 = id / (kGroupM * n_ot) * kGroupM, gsz = min(kGroupM, n_mt - gm0);
+  const int in = id - gm0 * n_ot;
+  const int64_t m0 = static_cast<int64_t>(gm0 + in % gsz) * kTM;
+  const int64_t o0 = static_cast<int64_t>(in / gsz) * kTO;
+
+  // piece p = tid + kThreads i: row p / 8, slot p % 8
+  const int rows_o = static_cast<int>(min(static_cast<int64_t>(kTO), a.O - o0));
+  const int rows_m = static_cast<int>(min(static_cast<int64_t>(kTM), a.M - m0));
+  const int nk = a.nk;
+  const Buf wb = make_buf(a.w + o0 * a.ldw, static_cast<int32_t>((rows_o - 1) * a.ldw) + 128 * nk, kSitePlanes, ig::kBufFlags);
+  const Buf qb = make_buf(a.q + m0 * a.ldq, static_cast<int32_t>((rows_m - 1) * a.ldq) + 128 * nk, kSiteActs, ig::kBufFlags);
+  uint32_t wp[kPO], qp[kPM];
+  const int prow = tid / 8, slot = tid % 8;
+#pragma unroll
+  for (int i = 0; i < kPO; ++i)
+    wp[i] = static_cast<uint32_t>(min(prow + kThreads / 8 * i, rows_o - 1)) * static_cast<uint32_t>(a.ldw) + 16 * slot;
+#pragma unroll
+  for (int i = 0; i < kPM; ++i)
+    qp[i] = static_cast<uint32_t>(min(prow + kThreads / 8 * i, rows_m - 1)) * static_cast<uint32_t>(a.ldq) + 16 * slot;
+  // rows prow + a multiple of 32: the swizzles repeat
+  const int wat = w_off(prow, slot), qat = q_off(prow, slot);
+  v4i rw[kPO], rq[kPM];
+  auto fetch = [&](int s) {
+    const int k = 128 * min(s * kG + grp, nk - 1);
+    // a group without a step of its own at the end reads zero weights
+    const uint32_t none = kG > 1 && s * kG + grp >= nk ? ig::kOutOfRange : 0u;
+#pragma unroll
+    for (int i = 0; i < kPO; ++i) rw[i] = buf_load_b128(wb, wp[i] | none, k);
+#pragma unroll
+    for (int i = 0; i < kPM; ++i) rq[i] = buf_load_b128(qb, qp[i], k);
+  };
+  auto publish = [&](int st) {
+    unsigned char* b = lds + st * kStage;
+#pragma unroll
+    for (int i = 0; i < kPO; ++i) *reinterpret_cast<v4i*>(b + wat + kThreads * 16 * i) = rw[i];
+#pragma unroll
+    for (int i = 0; i < kPM; ++i) *reinterpret_cast<v4i*>(b + kTO * 128 + qat + kThreads * 16 * i) = rq[i];
+  };
+  // fragment j of 32 bytes of k: lane l has row l % 32, bytes 32 j + 16 (l / 32)
+  const int wo = (wave % kWO) * 32 * kBO, wm = (wave / kWO) * 32 * kBM;
+  v4i fw[2][kBO], fq[2][kBM];
+  auto frags = [&](int st, int j, int u) {
+    const unsigned char* b = lds + st * kStage;
+    const int wl = w_off(wo + order(lane % 32), 2 * j + lane / 32), ql = q_off(wm + lane % 32, 2 * j + lane / 32);
+#pragma unroll
+    for (int i = 0; i < kBO; ++i) fw[u][i] = *reinterpret_cast<const v4i*>(b + wl + 4096 * i);
+#pragma unroll
+    for (int i = 0; i < kBM; ++i) fq[u][i] = *reinterpret_cast<const v4i*>(b + kTO * 128 + ql + 4096 * i);
+  };
+  v16i acc[kBO][kBM];
+#pragma unroll
+  for (int i = 0; i < kBO; ++i)
+#pragma unroll
+    for (int j = 0; j < kBM; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0;
+  auto products = [&](int u) {
+#pragma unroll
+    for (int i = 0; i < kBO; ++i)
+#pragma unroll
+      for (int j = 0; j < kBM; ++j)
+        acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fw[u][i], fq[u][j], acc[i][j], 0, 0, 0);
+  };
+
+  // Past the last step the fetch is of it again and the other stage gets what
+  // nobody reads, so that a step is one basic block.
+  const int ns = (nk + kG - 1) / kG;
+  fetch(0);
+  publish(0);
+  fetch(1);
+  __syncthreads();
+  frags(0, 0, 0);
+  for (int s = 0; s < ns; ++s) {
+    const int st = s & 1;
+    frags(st, 1, 1);
+    products(0);
+    interleave<kBO * kBM, kBO + kBM, 0, 0>();
+    frags(st, 2, 0);
+    products(1);
+    publish(st ^ 1);
+    interleave<kBO * kBM, kBO + kBM, kPO + kPM, 0x200>();
+    fetch(s + 2);
+    frags(st, 3, 1);
+    products(0);
+    interleave<kBO * kBM, kBO + kBM, kPO + kPM, 0x20>();
+    __syncthreads();
+    frags(st ^ 1, 0, 0);
+    products(1);
+    interleave<kBO * kBM, kBO + kBM, 0, 0>();
+  }
+
+  if constexpr (kG > 1) {
+    // the groups' sums, added in order by the first (the last step's other
+    // stage may still be written when the loop ends, hence the barrier)
+    constexpr int kRed = kBO * kBM * 4 * kThreads;  // 16-byte pieces a group
+    static_assert((kG - 1) * kRed * 16 <= kG * 2 * kStage, "");
+    v4i* red = reinterpret_cast<v4i*>(lds_all);
+    __syncthreads();
+    if (grp > 0)
+#pragma unroll
+      for (int i = 0; i < kBO; ++i)
+#pragma unroll
+        for (int j = 0; j < kBM; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            red[(grp - 1) * kRed + ((i * kBM + j) * 4 + e) * kThreads + tid] =
+                v4i{acc[i][j][4 * e], acc[i][j][4 * e + 1], acc[i][j][4 * e + 2], acc[i][j][4 * e + 3]};
+    __syncthreads();
+    if (grp > 0) return;
+#pragma unroll
+    for (int h = 0; h < kG - 1; ++h)
+#pragma unroll
+      for (int i = 0; i < kBO; ++i)
+#pragma unroll
+        for (int j = 0; j < kBM; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const v4i r = red[h * kRed + ((i * kBM + j) * 4 + e) * kThreads + tid];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) acc[i][j][4 * e + c] += r[c];
+          }
+  }
+
+  // epilogue: a lane has row l % 32 of a block and channels 16 (l / 32) + [0, 16)
+#pragma unroll
+  for (int i = 0; i < kBO; ++i) {
+    const int64_t o = o0 + wo + 32 * i + 16 * (lane / 32);
+    if (o >= a.O) continue;
+    float sw[16], bs[16];
+#pragma unroll
+    for (int c = 0; c < 16; ++c) {
+      const int64_t oc = min(o + c, static_cast<int64_t>(a.O) - 1);
+      sw[c] = a.sw[oc];
+      bs[c] = a.bias ? a.bias[oc] : 0.0f;
+    }
+#pragma unroll
+    for (int j = 0; j < kBM; ++j) {
+      const int64_t m = m0 + wm + 32 * j + lane % 32;
+      if (m >= a.M) continue;
+      const float sx = a.sx[m];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        float v[8];
+#pragma unroll
+        for (int c = 0; c < 8; ++c) v[c] = scaled(acc[i][j][8 * h + c], sx, sw[8 * h + c], bs[8 * h + c]);
+        put8<kType>(a, m, o + 8 * h, v);
+      }
+    }
+  }
+}
+
+template <int kWO, int kWM, int kBO, int kBM, int kG, int kType>
+fgq_status launch_tile(const I8Args& a, hipStream_t st) {
+  const int64_t n_mt = ceil_div(a.M, 32 * kWM * kBM), n_ot = ceil_div(a.O, 32 * kWO * kBO);
+  if (n_mt * n_ot >= (1LL << 31)) return FGQ_ERR_UNSUPPORTED;
+  hipLaunchKernelGGL((i8_tile_kernel<kWO, kWM, kBO, kBM, kG, kType>), dim3(static_cast<uint32_t>(n_mt * n_ot)),
+                     dim3(64 * kWO * kWM * kG), 0, st, a, static_cast<int>(n_mt), static_cast<int>(n_ot));
+  return last_launch();
+}
+
+}  // namespace
+
+fgq_status launch_i8_tile(const I8Args& a, Tile tile, int32_t y_type, hipStream_t st) {
+  return with_type(y_type, [&](auto t) {
+    constexpr int kType = decltype(t)::value;
+    switch (tile) {
+      case kTile256: return launch_tile<2, 4, 4, 2, 1, kType>(a, st);
+      case kTile128: return launch_tile<2, 2, 2, 2, 1, kType>(a, st);
+      case kTile128x2: return launch_tile<2, 2, 2, 2, 2, kType>(a, st);
+      case kTile64by128x2: return launch_tile<2, 2, 2, 1, 2, kType>(a, st);
+      case kTile64x2: return launch_tile<2, 2, 1, 1, 2, kType>(a, st);
+      default: return launch_tile<2, 2, 1, 1, 4, kType>(a, st);
+    }
+  });
+}
+
+}  // namespace fgq

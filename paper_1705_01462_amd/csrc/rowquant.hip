@@ -13,7 +13,9 @@
 namespace fgq {
 namespace {
 
-constexpr int kThreads = 256;
+// Eights of a row a thread keeps in registers between the maximum and the
+// codes (more are read again).
+constexpr int kKeep = 4;
 
 struct RowArgs {
   const void* x;
@@ -22,23 +24,29 @@ struct RowArgs {
   float* scale;
 };
 
-template <int kType>
+template <int kType, int kThreads>
 __global__ __launch_bounds__(kThreads) void quantize_rows_kernel(RowArgs a) {
   __shared__ uint32_t red[kThreads / 64];
   const int tid = threadIdx.x;
   const int64_t row = blockIdx.x;
   const char* x = static_cast<const char*>(a.x) + row * a.ldx * Elem<kType>::kBytes;
-  uint32_t m = 0;
-  for (int64_t k = 8 * tid; k < a.K; k += 8 * kThreads) {
-    if (k + 8 <= a.K) {
-      float v[8];
-      values8<kType>(load8<kType>(x, k), v);
+  const int64_t whole = a.K / 8;
+  Raw8<kType> keep[kKeep];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) m = max(m, abs_bits(v[j]));
-    } else {
-      for (int64_t j = k; j < a.K; ++j) m = max(m, abs_bits(Elem<kType>::get(x, j)));
-    }
-  }
+  for (int j = 0; j < kKeep; ++j)
+    if (tid + kThreads * j < whole) keep[j] = load8<kType>(x, 8LL * (tid + kThreads * j));
+  uint32_t m = 0;
+  auto add = [&](const Raw8<kType>& k) {
+    float v[8];
+    values8<kType>(k, v);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) m = max(m, abs_bits(v[j]));
+  };
+#pragma unroll
+  for (int j = 0; j < kKeep; ++j)
+    if (tid + kThreads * j < whole) add(keep[j]);
+  for (int64_t p = tid + kThreads * kKeep; p < whole; p += kThreads) add(load8<kType>(x, 8 * p));
+  if (tid < a.K - 8 * whole) m = max(m, abs_bits(Elem<kType>::get(x, 8 * whole + tid)));
   m = wave_max(m);
   if (tid % 64 == 0) red[tid / 64] = m;
   __syncthreads();
@@ -47,17 +55,28 @@ __global__ __launch_bounds__(kThreads) void quantize_rows_kernel(RowArgs a) {
   const RowScale s = row_scale(m);
   if (tid == 0 && check_store(kSiteStoreQ, row, 1, a.M)) a.scale[row] = s.scale;
   int8_t* q = a.q + row * a.ldq;
-  const int64_t Kp = round_up(a.K, kI8RowStep);
-  for (int64_t k = 8 * tid; k < Kp; k += 8 * kThreads) {
-    float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (k + 8 <= a.K) {
-      values8<kType>(load8<kType>(x, k), v);
-    } else {
-      for (int j = 0; j < 8; ++j)
-        if (k + j < a.K) v[j] = Elem<kType>::get(x, k + j);
+  auto put = [&](int64_t p, const float (&v)[8]) {
+    if (check_store(kSiteStoreQ, row * a.ldq + 8 * p, 8, a.M * a.ldq))
+      *reinterpret_cast<uint64_t*>(q + 8 * p) = row_codes8(v, s);
+  };
+#pragma unroll
+  for (int j = 0; j < kKeep; ++j)
+    if (tid + kThreads * j < whole) {
+      float v[8];
+      values8<kType>(keep[j], v);
+      put(tid + kThreads * j, v);
     }
-    if (check_store(kSiteStoreQ, row * a.ldq + k, 8, a.M * a.ldq))
-      *reinterpret_cast<uint64_t*>(q + k) = row_codes8(v, s);
+  for (int64_t p = tid + kThreads * kKeep; p < whole; p += kThreads) {
+    float v[8];
+    values8<kType>(load8<kType>(x, 8 * p), v);
+    put(p, v);
+  }
+  // the last values and the zeros up to the next multiple of kI8RowStep
+  if (const int64_t p = whole + tid; p < round_up(a.K, kI8RowStep) / 8) {
+    float v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = 8 * p + j < a.K ? Elem<kType>::get(x, 8 * p + j) : 0.0f;
+    put(p, v);
   }
 }
 
@@ -67,8 +86,12 @@ fgq_status launch_quantize_rows(const void* x, int32_t type, int64_t M, int64_t 
                                 int64_t ldq, float* scale, hipStream_t st) {
   const RowArgs a{x, M, K, ldx, ldq, q, scale};
   return with_type(type, [&](auto t) {
-    hipLaunchKernelGGL((quantize_rows_kernel<decltype(t)::value>), dim3(static_cast<uint32_t>(M)), dim3(kThreads), 0,
-                       st, a);
+    // A long row is a chain of loads for 256 threads; 1024 make it one round.
+    constexpr int kType = decltype(t)::value;
+    if (K > 256 * 8 * kKeep)
+      hipLaunchKernelGGL((quantize_rows_kernel<kType, 1024>), dim3(static_cast<uint32_t>(M)), dim3(1024), 0, st, a);
+    else
+      hipLaunchKernelGGL((quantize_rows_kernel<kType, 256>), dim3(static_cast<uint32_t>(M)), dim3(256), 0, st, a);
     return last_launch();
   });
 }
