@@ -109,7 +109,8 @@ int32_t fgq_abi_version(void);
  * kind of access and the byte or element offset of the first: 1
  * activations, 2 weight planes, 3 codes, 4 scale bytes, 5 group scales,
  * 6 offset terms, 7 partial maxima, 8 layer outputs, 9 split-K sums, 10
- * activation codes, 11 key/value cache), and clears the counts.  For testing, not for
+ * activation codes, 11 and 12 stores to and loads from a key/value cache),
+ * and clears the counts.  For testing, not for
  * production: the normal library (libfgq.so) returns FGQ_ERR_UNSUPPORTED.
  * FGQ_ERR_NULL if count is NULL; FGQ_ERR_HIP on a runtime error.
  */

@@ -35,7 +35,8 @@ enum CheckSite : uint32_t {
   kSiteStoreY = 8,    // layer outputs (fp32 or codes)
   kSiteStorePart = 9, // split-K int32 sums
   kSiteStoreQ = 10,   // quantized activation codes
-  kSiteStoreCache = 11,  // codes and parameters of a key/value cache
+  kSiteStoreCache = 11,  // stores to a key/value cache
+  kSiteCache = 12,    // its bytes as the attention reads them
 };
 
 #ifdef FGQ_CHECK

@@ -120,6 +120,10 @@ __device__ inline void store8(void* p, int64_t i, const float (&v)[8]) {
   for (int j = 0; j < Raw8<kType>::kN; ++j) d[j] = pk{r.w[j].x, r.w[j].y, r.w[j].z, r.w[j].w};
 }
 
+// Lanes of a wave exchange data through LDS: the compiler keeps the accesses
+// in this order, and the hardware does for the accesses of one wave.
+__device__ inline void wave_fence() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
+
 // fn(integral_constant<type>) for a type that was validated.
 template <typename F>
 inline auto with_type(int32_t type, F&& fn) {

@@ -33,10 +33,6 @@ constexpr int kAheadFor = kMB <= 2 ? 4 : 3;
 // 16 consecutive rows) touch every bank once.
 __device__ inline int frag_off(int row, int slot) { return row * 128 + 16 * (slot ^ ((row & 7) ^ (row >> 3 & 1))); }
 
-// Lanes of a wave exchange data through LDS: the compiler keeps the accesses
-// in this order, and the hardware does for the accesses of one wave.
-__device__ inline void wave_fence() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
-
 template <int kMB, int kXType, int kType>
 __global__ __launch_bounds__(kThreads, 1) void i8_few_kernel(I8Args a, const void* x, int64_t ldx, int64_t K) {
   constexpr bool kFused = kXType >= 0;

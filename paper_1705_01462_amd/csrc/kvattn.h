@@ -8,6 +8,10 @@
 
 namespace fgq {
 
+// Keys of a split are a multiple of kKvAttnSplit (every wave's steps, of at
+// most kKvAttnAlign keys, are whole in it).
+constexpr int kKvAttnAlign = 64, kKvAttnSplit = 256;
+
 struct KvAttnArgs {
   const void* q;           // [T][Hq][D], strides in elements
   int64_t q_st, q_sh;

@@ -11,37 +11,81 @@ namespace {
 
 constexpr int kJoinThreads = 256;
 
-// One wave a row: the splits' outputs, each divided by nothing yet, weighted
-// by 2^(its maximum - the largest), over the sum of the weighted sums.  The
-// order of the splits is fixed.
-template <int kType>
+// A workgroup a row: the splits' outputs weighted by 2^(their maximum - the
+// largest), over the sum of the weighted sums.  Each wave takes every fourth
+// split, several in flight; the order of the additions is fixed.
+template <int kType, int kD>
 __global__ __launch_bounds__(kJoinThreads) void kv_attn_join_kernel(KvAttnArgs a) {
-  const int lane = threadIdx.x % 64;
-  const int64_t item = static_cast<int64_t>(blockIdx.x) * (kJoinThreads / 64) + threadIdx.x / 64;
-  if (item >= static_cast<int64_t>(a.B) * a.max_q * a.Hq) return;
+  constexpr int kWaves = kJoinThreads / 64, kC = kD / 64, kAhead = 4;
+  typedef float vec __attribute__((ext_vector_type(kC), aligned(4)));
+  __shared__ float smax[kWaves], ssum[kWaves], so[kWaves][kD];
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  const int64_t item = blockIdx.x;
   const int head = static_cast<int>(item % a.Hq);
   const int i = static_cast<int>(item / a.Hq % a.max_q), b = static_cast<int>(item / a.Hq / a.max_q);
   const int64_t q0 = max(0, min(a.cu_q[b], static_cast<int>(a.T)));
   const int64_t q1 = max(q0, min(static_cast<int64_t>(a.cu_q[b + 1]), a.T));
   if (i >= q1 - q0) return;
   const int64_t row = (q0 + i) * a.Hq + head;
-  const float* p = a.part + row * a.splits * (a.D + 2);
+  const float* p = a.part + row * a.splits * (kD + 2);
+  // this lane's split of each 64: maxima and sums
   float mx = -INFINITY;
-  for (int s = 0; s < a.splits; ++s) mx = fmaxf(mx, p[s * (a.D + 2) + a.D]);
+  for (int s = threadIdx.x; s < a.splits; s += kJoinThreads) mx = fmaxf(mx, p[s * (kD + 2) + kD]);
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) mx = fmaxf(mx, __shfl_xor(mx, off));
+  if (lane == 0) smax[wave] = mx;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) mx = fmaxf(mx, smax[w]);
   const float base = mx == -INFINITY ? 0.0f : mx;
-  float sum = 0.0f, v[4] = {0, 0, 0, 0};
-  for (int s = 0; s < a.splits; ++s) {
-    const float* ps = p + s * (a.D + 2);
-    const float w = exp2f(ps[a.D] - base);
-    sum += w * ps[a.D + 1];
-    for (int j = 0; j < a.D / 64; ++j) v[j] += w * ps[64 * j + lane];
+  float sum = 0.0f;
+  vec v = {};
+  for (int s0 = wave; s0 < a.splits; s0 += kWaves * kAhead) {
+    vec o[kAhead];
+    float m[kAhead], l[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int s = min(s0 + kWaves * u, a.splits - 1);
+      const float* ps = p + static_cast<int64_t>(s) * (kD + 2);
+      o[u] = *reinterpret_cast<const vec*>(ps + kC * lane);
+      m[u] = ps[kD];
+      l[u] = ps[kD + 1];
+    }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+      if (s0 + kWaves * u < a.splits) {
+        const float w = exp2f(m[u] - base);
+        sum += w * l[u];
+        v += w * o[u];
+      }
   }
-  for (int j = 0; j < a.D / 64; ++j) {
-    const int64_t at = row * a.D + 64 * j + lane;
-    if (check_store(kSiteStoreY, at, 1, a.T * a.Hq * a.D)) Elem<kType>::put(a.o, at, sum == 0.0f ? 0.0f : v[j] / sum);
+  if (lane == 0) ssum[wave] = sum;
+#pragma unroll
+  for (int c = 0; c < kC; ++c) so[wave][kC * lane + c] = reinterpret_cast<const float*>(&v)[c];
+  __syncthreads();
+  sum = 0.0f;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) sum += ssum[w];
+  if (threadIdx.x < kD) {
+    float x = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) x += so[w][threadIdx.x];
+    const int64_t at = row * kD + threadIdx.x;
+    if (check_store(kSiteStoreY, at, 1, a.T * a.Hq * kD)) Elem<kType>::put(a.o, at, sum == 0.0f ? 0.0f : x / sum);
   }
-  if (lane == 0 && a.lse && check_store(kSiteStoreY, row, 1, a.T * a.Hq))
+  if (threadIdx.x == 0 && a.lse && check_store(kSiteStoreY, row, 1, a.T * a.Hq))
     a.lse[row] = sum > 0.0f ? (mx + log2f(sum)) * 0.6931471805599453f : (sum == 0.0f ? -INFINITY : sum);
+}
+
+template <int kType>
+void launch_join(const KvAttnArgs& a, int64_t items, hipStream_t st) {
+  const dim3 grid(static_cast<uint32_t>(items)), wg(kJoinThreads);
+  if (a.D == 64)
+    hipLaunchKernelGGL((kv_attn_join_kernel<kType, 64>), grid, wg, 0, st, a);
+  else if (a.D == 128)
+    hipLaunchKernelGGL((kv_attn_join_kernel<kType, 128>), grid, wg, 0, st, a);
+  else
+    hipLaunchKernelGGL((kv_attn_join_kernel<kType, 256>), grid, wg, 0, st, a);
 }
 
 struct Plan {
@@ -49,31 +93,38 @@ struct Plan {
   bool share;
 };
 
-Plan plan(int32_t Hq, int32_t Hkv, int64_t B, int64_t max_q, int64_t max_keys) {
+// max_keys: the most keys of a sequence, as far as the host knows.  Three
+// workgroups fit a unit, so keys are split until there are that many (us, two
+// sequences of 131072 keys and 16 (sequence, key head) pairs: 1.5 a unit 89, 3
+// 72, 6 80, 12 89; 48 sequences of up to 8191: 90, 82, 91, 99), but not below
+// 512 keys, which four waves step through a few times.
+Plan plan(int32_t Hq, int32_t Hkv, int64_t B, int64_t max_q, int64_t max_keys, int64_t window) {
   Plan p{};
   const int64_t rows = max_q * (Hq / Hkv);
   p.share = rows <= 64;
   p.nt = rows <= 16 ? 1 : 2;
   p.tiles = static_cast<int>(ceil_div(rows, 16 * p.nt * (p.share ? 1 : 4)));
+  // keys that a tile's rows can see, and its first step's alignment
+  const int64_t keys = (window ? std::min(max_keys, window + max_q) : max_keys) + kKvAttnAlign;
   p.splits = 1;
   if (p.share) {
-    const int64_t wgs = B * Hkv * p.tiles, want = 8LL * ig::device_cus();
-    const int64_t most = ceil_div(max_keys, 512);
-    p.splits = static_cast<int>(std::max<int64_t>(1, std::min({most, ceil_div(want, wgs), int64_t{256}})));
+    const int64_t wgs = B * Hkv * p.tiles, want = 3LL * ig::device_cus();
+    p.splits = static_cast<int>(std::max<int64_t>(1, std::min({keys / kKvAttnSplit, want / wgs, int64_t{1024}})));
   }
-  p.split_keys = static_cast<int>(round_up(ceil_div(max_keys + 15, p.splits), 512));
+  p.split_keys = static_cast<int>(round_up(ceil_div(keys, p.splits), kKvAttnSplit));
+  p.splits = static_cast<int>(ceil_div(keys, p.split_keys));
   return p;
 }
 
 }  // namespace
 
 size_t kv_attn_ws_bytes(int64_t T, int32_t Hq, int32_t Hkv, int32_t D, int64_t B, int64_t max_q, int64_t max_keys) {
-  const Plan p = plan(Hq, Hkv, B, max_q, max_keys);
+  const Plan p = plan(Hq, Hkv, B, max_q, max_keys, 0);
   return p.splits == 1 ? 0 : static_cast<size_t>(T) * Hq * p.splits * (D + 2) * sizeof(float);
 }
 
 fgq_status launch_kv_attn(KvAttnArgs a, void* ws, hipStream_t st) {
-  const Plan p = plan(a.Hq, a.Hkv, a.B, a.max_q, a.max_pages * a.P);
+  const Plan p = plan(a.Hq, a.Hkv, a.B, a.max_q, a.max_pages * a.P, a.window);
   a.tiles = p.tiles;
   a.splits = p.splits;
   a.split_keys = p.split_keys;
@@ -83,11 +134,10 @@ fgq_status launch_kv_attn(KvAttnArgs a, void* ws, hipStream_t st) {
                                      : launch_kv_attn_d256(a, p.nt, p.share, st);
   if (rc != FGQ_OK || p.splits == 1) return rc;
   const int64_t items = static_cast<int64_t>(a.B) * a.max_q * a.Hq;
-  const dim3 grid(static_cast<uint32_t>(ceil_div(items, kJoinThreads / 64)));
   if (a.type == FGQ_F16)
-    hipLaunchKernelGGL(kv_attn_join_kernel<FGQ_F16>, grid, dim3(kJoinThreads), 0, st, a);
+    launch_join<FGQ_F16>(a, items, st);
   else
-    hipLaunchKernelGGL(kv_attn_join_kernel<FGQ_BF16>, grid, dim3(kJoinThreads), 0, st, a);
+    launch_join<FGQ_BF16>(a, items, st);
   return last_launch();
 }
 

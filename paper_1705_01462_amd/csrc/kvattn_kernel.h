@@ -48,6 +48,12 @@ constexpr float kSlack = 4.0f;     // log2 of how far a score may pass its row's
 constexpr float kBoost = 2048.0f;  // 2^11: the largest rounded probability is 2^(4 + 11)
 constexpr int kAttnThreads = 256;
 constexpr int kAttnWaves = 4;
+#ifndef LB
+#define LB 2
+#endif
+#ifndef KT
+#define KT 2
+#endif
 
 __device__ inline kv8h frag(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   return __builtin_bit_cast(kv8h, ev4u{a, b, c, d});
@@ -91,6 +97,14 @@ __device__ inline uint32_t value_pair(uint32_t w, int n) {
   return __builtin_bit_cast(uint32_t, __builtin_bit_cast(v2h, c) + __builtin_bit_cast(v2h, mid));
 }
 
+// a * b, with 0 times anything (NaN, infinity) 0.  The wait state is for an a
+// that comes straight from v_exp_f32, which the compiler does not see in here.
+__device__ inline float mul_zero(float a, float b) {
+  float r;
+  asm("s_nop 0\n\tv_mul_legacy_f32 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+  return r;
+}
+
 // kNT: 16-row blocks a wave.  kShare: the four waves have the same rows and
 // divide the keys (and workgroups may too: splits); else each wave has rows of
 // its own and all the keys.  kKT: 16-key tiles a step (even).
@@ -109,14 +123,35 @@ struct KvAttn {
   static constexpr int kKeys = 16 * kKT;
   static constexpr int kPairs = kKT / 2;
 
+  static constexpr int kC = kRow / 16;                 // 16-byte chunks of a token
+  static constexpr int kLB = kRow / 4;                 // bytes of 16 tokens a lane loads
+  static constexpr int kLN = kLB >= 16 ? kLB / 16 : 1;
+  static constexpr int kPN = (32 * kNG + 63) / 64;     // parameters of 16 tokens a lane loads
+  // a wave's LDS: key codes, value codes, parameters [tile][k, v][group][16]
+  static constexpr int kTileB = 16 * kRow;
+  static constexpr int kVAt = kKT * kTileB, kPAt = 2 * kKT * kTileB, kWaveB = kPAt + kKT * 128 * kNG;
+  typedef typename std::conditional<kLB == 8, uint2, ev4u>::type piece;
+
+  // A step's bytes as they come from memory.
   struct Raw {
-    uint32_t k[kKT][kNG][kKW];
-    uint32_t v[kKT][4][kNG][kVB >= 4 ? kVB / 4 : 1];
-    ev4u kp[kKT][kNG], vp[kKT][kNG];
+    piece k[kKT][kLN], v[kKT][kLN];
+    uint32_t par[kKT][kPN];
   };
+
+  // LDS offset of a chunk of one of 16 tokens.  Swizzled: the fragment reads of
+  // eight consecutive tokens at one chunk, and the values' reads of whole tokens
+  // four apart, touch every bank once.
+  static __device__ int chunk_off(int row, int chunk) {
+    if constexpr (kC == 2) return (row >> 2) * 128 + 16 * (2 * ((row ^ row >> 2) & 3) + (chunk ^ (row >> 2 & 1)));
+    if constexpr (kC == 4)
+      return (row >> 1) * 128 + 16 * (4 * ((row ^ row >> 2) & 1) + (chunk ^ (row >> 1 & 3) ^ (row >> 3 & 1)));
+    return row * kRow + 16 * (chunk ^ (row & 7) ^ (row >> 3 & 1));
+  }
 
   const KvAttnArgs& a;
   int lane, c16, g;
+  unsigned char* mine;         // the wave's LDS
+  uint32_t poff[kPN];          // where this lane's parameters of 16 tokens lie
   const uint8_t* head;         // cache + this key head
   const int32_t* pg;           // the sequence's pages
   kv8h q[kNT][kNG][kSteps];
@@ -172,80 +207,129 @@ struct KvAttn {
     }
   }
 
-  // ---- one step's bytes.  last: the largest key whose page is known to be the sequence's own
+  // ---- one step's bytes: 16 tokens at a time, whole runs of a page.  last: the
+  // largest key whose page is known to be the sequence's own
   __device__ void load(Raw& r, int key0, int last) const {
-#pragma unroll
-    for (int t = 0; t < kKT; ++t) {
-      const int key = min(key0 + 16 * t, last & ~15);
+    // the bytes of this head in the page that holds `key`
+    auto page_of = [&](int key) {
       const int pid = __builtin_amdgcn_readfirstlane(pg[key >> a.pshift]);
       // a page number outside the cache reads page 0 instead of foreign memory
       const int64_t page = static_cast<uint32_t>(pid) < static_cast<uint32_t>(a.num_pages) ? pid : 0;
-      const uint8_t* base = head + page * a.page_bytes;
-      const int at = key & (a.P - 1);
-      const uint8_t* kb = base + at * kRow;
-      const uint8_t* vb = base + (a.P + at) * kRow;
-      const uint8_t* kp = base + 2 * a.P * kRow + 4 * at;
-      const uint8_t* vp = kp + 4 * kNG * a.P;
+      return make_buf(head + page * a.page_bytes, 2 * a.P * (kRow + 4 * kNG), kSiteCache, ig::kBufFlags);
+    };
+    auto tile = [&](const Buf& pgb, int t, int at) {
 #pragma unroll
-      for (int gr = 0; gr < kNG; ++gr) {
-        const uint8_t* p = kb + c16 * kRow + gr * kGB + g * (4 * kKW);
-        if constexpr (kKW == 1) {
-          r.k[t][gr][0] = *reinterpret_cast<const uint32_t*>(p);
-        } else if constexpr (kKW == 2) {
-          const uint2 w = *reinterpret_cast<const uint2*>(p);
-          r.k[t][gr][0] = w.x;
-          r.k[t][gr][1] = w.y;
-        } else {
+      for (int j = 0; j < kLN; ++j) {
+        r.k[t][j] = get(pgb, 1024 * j + static_cast<int>(sizeof(piece)) * lane, at * kRow);
+        r.v[t][j] = get(pgb, 1024 * j + static_cast<int>(sizeof(piece)) * lane, (a.P + at) * kRow);
+      }
 #pragma unroll
-          for (int j = 0; j < kKW / 4; ++j) {
-            const ev4u w = reinterpret_cast<const ev4u*>(p)[j];
+      for (int j = 0; j < kPN; ++j) r.par[t][j] = buf_load_b32(pgb, poff[j], 2 * a.P * kRow + 4 * at);
+    };
+    if (a.P >= kKeys) {  // steps are aligned to kKeys: one page
+      const int key = min(key0, last);
+      const Buf pgb = page_of(key);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) r.k[t][gr][4 * j + e] = w[e];
-          }
-        }
-        r.kp[t][gr] = *reinterpret_cast<const ev4u*>(kp + 4 * gr * a.P + 16 * g);
-        r.vp[t][gr] = *reinterpret_cast<const ev4u*>(vp + 4 * gr * a.P + 16 * g);
+      for (int t = 0; t < kKT; ++t) tile(pgb, t, (key0 & (a.P - 1)) + 16 * t);
+    } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const uint8_t* s = vb + (4 * g + i) * kRow + gr * kGB + c16 * kVB;
-          if constexpr (kVB == 1) {
-            r.v[t][i][gr][0] = *s;
-          } else if constexpr (kVB == 2) {
-            r.v[t][i][gr][0] = *reinterpret_cast<const uint16_t*>(s);
-          } else if constexpr (kVB == 4) {
-            r.v[t][i][gr][0] = *reinterpret_cast<const uint32_t*>(s);
-          } else {
-            const uint2 w = *reinterpret_cast<const uint2*>(s);
-            r.v[t][i][gr][0] = w.x;
-            r.v[t][i][gr][1] = w.y;
-          }
-        }
+      for (int t = 0; t < kKT; ++t) {
+        const int key = min(key0 + 16 * t, last & ~15);
+        tile(page_of(key), t, key & (a.P - 1));
+      }
+    }
+  }
+  static __device__ piece get(const Buf& b, uint32_t voff, uint32_t soff) {
+    if constexpr (kLB == 8) {
+      const bc_v2i x = buf_load_b64(b, voff, soff);
+      return uint2{static_cast<uint32_t>(x.x), static_cast<uint32_t>(x.y)};
+    } else {
+      return __builtin_bit_cast(ev4u, buf_load_b128(b, voff, soff));
+    }
+  }
+
+  // ---- into the wave's LDS
+  __device__ void stage(const Raw& r) const {
+#pragma unroll
+    for (int j = 0; j < kLN; ++j) {
+      const int byte = 1024 * j + static_cast<int>(sizeof(piece)) * lane;
+      const int off = chunk_off(byte / kRow, byte % kRow / 16) + byte % 16;
+#pragma unroll
+      for (int t = 0; t < kKT; ++t) {
+        *reinterpret_cast<piece*>(mine + t * kTileB + off) = r.k[t][j];
+        *reinterpret_cast<piece*>(mine + kVAt + t * kTileB + off) = r.v[t][j];
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < kPN; ++j)
+      if (32 * kNG % 64 == 0 || lane < 32)
+#pragma unroll
+        for (int t = 0; t < kKT; ++t)
+          *reinterpret_cast<uint32_t*>(mine + kPAt + t * 128 * kNG + 4 * (64 * j + lane)) = r.par[t][j];
+  }
+
+  __device__ ev4u params(int t, int z, int gr) const {
+    return *reinterpret_cast<const ev4u*>(mine + kPAt + 64 * ((t * 2 + z) * kNG + gr) + 16 * g);
+  }
+
+  // Words of a key's group (fragment row c16): kKW of them from word g kKW.
+  __device__ void key_words(int t, int gr, uint32_t (&w)[kKW]) const {
+    const int byte = gr * kGB + g * 4 * kKW;
+    if constexpr (kKW <= 4) {
+      const unsigned char* p = mine + t * kTileB + chunk_off(c16, byte / 16) + byte % 16;
+      if constexpr (kKW == 1) {
+        w[0] = *reinterpret_cast<const uint32_t*>(p);
+      } else if constexpr (kKW == 2) {
+        const uint2 x = *reinterpret_cast<const uint2*>(p);
+        w[0] = x.x;
+        w[1] = x.y;
+      } else {
+        const ev4u x = *reinterpret_cast<const ev4u*>(p);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = x[e];
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < kKW / 4; ++j) {
+        const ev4u x = *reinterpret_cast<const ev4u*>(mine + t * kTileB + chunk_off(c16, byte / 16 + j));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[4 * j + e] = x[e];
       }
     }
   }
 
-  // ---- one step.  kMask: some row does not see some of its keys
-  template <bool kMask>
-  __device__ void compute(const Raw& r, int key0) {
+  // The bytes of a value's group that this lane has, key 4 g + i of a tile.
+  typedef typename std::conditional<kVB == 1, uint8_t, typename std::conditional<
+      kVB == 2, uint16_t, typename std::conditional<kVB == 4, uint32_t, uint2>::type>::type>::type vpart;
+  __device__ vpart value_part(int t, int i, int gr) const {
+    const int byte = gr * kGB + c16 * kVB;
+    return *reinterpret_cast<const vpart*>(mine + kVAt + t * kTileB + chunk_off(4 * g + i, byte / 16) + byte % 16);
+  }
+
+  // ---- one step.  mask: some row does not see some of its keys
+  __device__ void compute(int key0, bool mask) {
     // scores, keys x rows
     kv4f S[kKT][kNT];
 #pragma unroll
     for (int t = 0; t < kKT; ++t) {
 #pragma unroll
       for (int gr = 0; gr < kNG; ++gr) {
+        uint32_t kw[kKW];
+        key_words(t, gr, kw);
+        const ev4u kp = params(t, 0, gr);
         kv4f d[kNT];
 #pragma unroll
         for (int n = 0; n < kNT; ++n) d[n] = kv4f{0, 0, 0, 0};
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) {
-          const kv8h kf = kBits == 4 ? key_frag<kBits>(r.k[t][gr][s], 0)
-                                     : key_frag<kBits>(r.k[t][gr][(2 * s) % kKW], r.k[t][gr][(2 * s + 1) % kKW]);
+          const kv8h kf = kBits == 4 ? key_frag<kBits>(kw[s % kKW], 0)
+                                     : key_frag<kBits>(kw[(2 * s) % kKW], kw[(2 * s + 1) % kKW]);
 #pragma unroll
           for (int n = 0; n < kNT; ++n) d[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, q[n][gr][s], d[n], 0, 0, 0);
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const float st = __uint_as_float(r.kp[t][gr][i] & 0xFFFF0000u), mn = bf16_f32(r.kp[t][gr][i]);
+          const float st = __uint_as_float(kp[i] & 0xFFFF0000u), mn = bf16_f32(kp[i]);
 #pragma unroll
           for (int n = 0; n < kNT; ++n)
             S[t][n][i] = gr == 0 ? fmaf(st, d[n][i], mn * qsum[n][gr])
@@ -253,7 +337,7 @@ struct KvAttn {
         }
       }
     }
-    if constexpr (kMask) {
+    if (mask) {
 #pragma unroll
       for (int t = 0; t < kKT; ++t)
 #pragma unroll
@@ -294,23 +378,41 @@ struct KvAttn {
       }
     }
     // largest steps
+    ev4u vp[kKT][kNG];
+#pragma unroll
+    for (int t = 0; t < kKT; ++t)
+#pragma unroll
+      for (int gr = 0; gr < kNG; ++gr) vp[t][gr] = params(t, 1, gr);
     float st[kNT][kNG];
+#pragma unroll
+    for (int gr = 0; gr < kNG; ++gr) {
+      float x = 0.0f;
+#pragma unroll
+      for (int t = 0; t < kKT; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x = fmaxf(x, __uint_as_float(vp[t][gr][i] & 0xFFFF0000u));
+#pragma unroll
+      for (int n = 0; n < kNT; ++n) st[n][gr] = x;
+    }
+    if (mask) {  // only of the keys that the row sees
+#pragma unroll
+      for (int gr = 0; gr < kNG; ++gr)
+#pragma unroll
+        for (int n = 0; n < kNT; ++n) {
+          float x = 0.0f;
+#pragma unroll
+          for (int t = 0; t < kKT; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              x = fmaxf(x, S[t][n][i] != -INFINITY ? __uint_as_float(vp[t][gr][i] & 0xFFFF0000u) : 0.0f);
+          st[n][gr] = x;
+        }
+    }
     bool grow = false;
 #pragma unroll
-    for (int gr = 0; gr < kNG; ++gr)
+    for (int n = 0; n < kNT; ++n)
 #pragma unroll
-      for (int n = 0; n < kNT; ++n) {
-        float x = 0.0f;
-#pragma unroll
-        for (int t = 0; t < kKT; ++t)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float s = __uint_as_float(r.vp[t][gr][i] & 0xFFFF0000u);
-            x = fmaxf(x, !kMask || S[t][n][i] != -INFINITY ? s : 0.0f);
-          }
-        st[n][gr] = x;
-        grow |= x > lim[n][gr];
-      }
+      for (int gr = 0; gr < kNG; ++gr) grow |= st[n][gr] > lim[n][gr];
     if (__any(grow)) {
 #pragma unroll
       for (int n = 0; n < kNT; ++n)
@@ -347,22 +449,17 @@ struct KvAttn {
         float vs[4], vl[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          vs[i] = __uint_as_float(r.vp[t][gr][i] & 0xFFFF0000u);
-          vl[i] = fmaf(vs[i], static_cast<float>(kMidCode<kBits>), bf16_f32(r.vp[t][gr][i]));
+          vs[i] = __uint_as_float(vp[t][gr][i] & 0xFFFF0000u);
+          vl[i] = fmaf(vs[i], static_cast<float>(kMidCode<kBits>), bf16_f32(vp[t][gr][i]));
         }
 #pragma unroll
         for (int n = 0; n < kNT; ++n) {
           float y[4];
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            y[i] = pr[n][i] * nrm[n][gr] * vs[i];
-            float z = pr[n][i] * vl[i];
-            if constexpr (kMask) {  // a hidden key's parameters may be NaN
-              const bool see = S[t][n][i] != -INFINITY;
-              y[i] = see ? y[i] : 0.0f;
-              z = see ? z : 0.0f;
-            }
-            losum[n][gr] += z;
+            // 0 times anything is 0: a hidden key's parameters may be NaN
+            y[i] = mul_zero(pr[n][i] * nrm[n][gr], vs[i]);
+            losum[n][gr] += mul_zero(pr[n][i], vl[i]);
           }
           p[t / 2][gr][n][2 * (t % 2)] = pack_f16(y[0], y[1]);
           p[t / 2][gr][n][2 * (t % 2) + 1] = pack_f16(y[2], y[3]);
@@ -374,22 +471,23 @@ struct KvAttn {
     for (int u = 0; u < kPairs; ++u)
 #pragma unroll
       for (int gr = 0; gr < kNG; ++gr) {
-        kv8h pf[kNT];
+            kv8h pf[kNT];
 #pragma unroll
         for (int n = 0; n < kNT; ++n) pf[n] = frag(p[u][gr][n][0], p[u][gr][n][1], p[u][gr][n][2], p[u][gr][n][3]);
         uint32_t w[4][kVP];  // key pairs (0,1) (2,3) of both tiles
 #pragma unroll
         for (int h = 0; h < 4; ++h) {
-          const auto& x = r.v[2 * u + h / 2][2 * (h % 2)][gr];
-          const auto& y = r.v[2 * u + h / 2][2 * (h % 2) + 1][gr];
+          const vpart x = value_part(2 * u + h / 2, 2 * (h % 2), gr), y = value_part(2 * u + h / 2, 2 * (h % 2) + 1, gr);
           if constexpr (kVB <= 2) {
-            w[h][0] = x[0] | y[0] << 16;
+            w[h][0] = static_cast<uint32_t>(x) | static_cast<uint32_t>(y) << 16;
+          } else if constexpr (kVB == 4) {
+            w[h][0] = __builtin_amdgcn_perm(y, x, 0x05040100u);
+            w[h][1] = __builtin_amdgcn_perm(y, x, 0x07060302u);
           } else {
-#pragma unroll
-            for (int j = 0; j < kVB / 4; ++j) {
-              w[h][2 * j] = __builtin_amdgcn_perm(y[j], x[j], 0x05040100u);
-              w[h][2 * j + 1] = __builtin_amdgcn_perm(y[j], x[j], 0x07060302u);
-            }
+            w[h][0] = __builtin_amdgcn_perm(y.x, x.x, 0x05040100u);
+            w[h][1] = __builtin_amdgcn_perm(y.x, x.x, 0x07060302u);
+            w[h][2 % kVP] = __builtin_amdgcn_perm(y.y, x.y, 0x05040100u);
+            w[h][3 % kVP] = __builtin_amdgcn_perm(y.y, x.y, 0x07060302u);
           }
         }
 #pragma unroll
@@ -426,12 +524,18 @@ struct KvAttn {
     }
   }
 
-  __device__ void run() {
+  __device__ void run(unsigned char* lds) {
     const int tid = threadIdx.x;
     lane = tid % 64;
     c16 = lane % 16;
     g = lane / 16;
     const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
+    mine = lds + wave * kWaveB;
+#pragma unroll
+    for (int j = 0; j < kPN; ++j) {
+      const int i = min(64 * j + lane, 32 * kNG - 1);  // [k, v][group][16]
+      poff[j] = 4 * (i / 16 * a.P + i % 16);
+    }
     // neighbouring workgroups of one sequence and head share its pages in an XCD's L2
     int id = ig::xcd_swizzle(blockIdx.x, gridDim.x);
     const int split = id % a.splits;
@@ -454,7 +558,7 @@ struct KvAttn {
     pg = a.pages + b * a.max_pages;
     const int rl = min(row0 + kRows, rows) - 1;  // last row
     // keys that some row sees, and keys that all rows see
-    int k0 = first_key(row0) & ~15, k1 = end_key(rl);
+    int k0 = first_key(row0) & ~(kKeys - 1), k1 = end_key(rl);
     const int all0 = first_key(rl), all1 = end_key(row0);
     if (a.splits > 1) {
       k0 += split * a.split_keys;
@@ -480,16 +584,17 @@ struct KvAttn {
     const int first = k0 + (kShare ? wave * kKeys : 0), hop = kShare ? kAttnWaves * kKeys : kKeys;
     const int last = k1 - 1;
     Raw r;
+    if (first < k1) load(r, first, last);
     for (int key = first; key < k1; key += hop) {
-      load(r, key, last);
-      if (key >= all0 && key + kKeys <= min(all1, k1))
-        compute<false>(r, key);
-      else
-        compute<true>(r, key);
+      stage(r);
+      if (key + hop < k1) load(r, key + hop, last);
+      wave_fence();
+      compute(key, key < all0 || key + kKeys > min(all1, k1));
+      wave_fence();
     }
     finish();
     if constexpr (kShare)
-      join(split, rows, row0, q0, h, wave);
+      join(lds, split, rows, row0, q0, h, wave);
     else
       store(rows, row0, q0, h);
   }
@@ -536,11 +641,16 @@ struct KvAttn {
   }
 
   // ---- the waves' parts of the same rows, 64 / kNT channels a round
-  __device__ void join(int split, int rows, int row0, int64_t q0, int h, int wave) {
+  // LDS: [wave][row] maxima and sums, then [wave][tile][row][16] outputs
+  static constexpr int kJoinB = 2 * kAttnWaves * kRows * 4 + kAttnWaves * (8 / kNT) * kRows * 64;
+  static constexpr int kLdsB = kShare && kJoinB > kAttnWaves * kWaveB ? kJoinB : kAttnWaves * kWaveB;
+  __device__ void join(unsigned char* lds, int split, int rows, int row0, int64_t q0, int h, int wave) {
     constexpr int kTiles = 8 / kNT;                   // accumulator tiles a round
     constexpr int kRounds = (kD / 16 + kTiles - 1) / kTiles;
-    __shared__ float sm[kAttnWaves][kRows], sl[kAttnWaves][kRows];
-    __shared__ float so[kAttnWaves][kTiles][kRows][16];
+    float(*sm)[kRows] = reinterpret_cast<float(*)[kRows]>(lds);
+    float(*sl)[kRows] = sm + kAttnWaves;
+    float(*so)[kTiles][kRows][16] = reinterpret_cast<float(*)[kTiles][kRows][16]>(lds + 2 * kAttnWaves * kRows * 4);
+    __syncthreads();  // the waves' own stages end here
     if (g == 0)
 #pragma unroll
       for (int n = 0; n < kNT; ++n) {
@@ -610,14 +720,16 @@ struct KvAttn {
 };
 
 template <int kBits, int kD, int kG, int kNT, bool kShare, int kKT>
-__global__ __launch_bounds__(kAttnThreads) void kv_attn_kernel(KvAttnArgs a) {
-  KvAttn<kBits, kD, kG, kNT, kShare, kKT> k(a);
-  k.run();
+__global__ __launch_bounds__(kAttnThreads, LB) void kv_attn_kernel(KvAttnArgs a) {
+  typedef KvAttn<kBits, kD, kG, kNT, kShare, kKT> K;
+  __shared__ __attribute__((aligned(16))) unsigned char lds[K::kLdsB];
+  K k(a);
+  k.run(lds);
 }
 
 template <int kBits, int kD, int kG>
 fgq_status launch_one(const KvAttnArgs& a, int nt, bool share, hipStream_t st) {
-  constexpr int kKT = 2;
+  constexpr int kKT = kD * kBits <= 512 && kD == kG ? 4 : 2;
   const dim3 grid(static_cast<uint32_t>(static_cast<int64_t>(a.B) * a.Hkv * a.tiles * a.splits)), wg(kAttnThreads);
   if (share && nt == 1)
     hipLaunchKernelGGL((kv_attn_kernel<kBits, kD, kG, 1, true, kKT>), grid, wg, 0, st, a);
