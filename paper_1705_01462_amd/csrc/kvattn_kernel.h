@@ -48,9 +48,6 @@ constexpr float kSlack = 4.0f;     // log2 of how far a score may pass its row's
 constexpr float kBoost = 2048.0f;  // 2^11: the largest rounded probability is 2^(4 + 11)
 constexpr int kAttnThreads = 256;
 constexpr int kAttnWaves = 4;
-#ifndef LB
-#define LB 2
-#endif
 #ifndef KT
 #define KT 2
 #endif
@@ -95,14 +92,6 @@ __device__ inline uint32_t value_pair(uint32_t w, int n) {
     mid = 0x80808080u;
   }
   return __builtin_bit_cast(uint32_t, __builtin_bit_cast(v2h, c) + __builtin_bit_cast(v2h, mid));
-}
-
-// a * b, with 0 times anything (NaN, infinity) 0.  The wait state is for an a
-// that comes straight from v_exp_f32, which the compiler does not see in here.
-__device__ inline float mul_zero(float a, float b) {
-  float r;
-  asm("s_nop 0\n\tv_mul_legacy_f32 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
-  return r;
 }
 
 // kNT: 16-row blocks a wave.  kShare: the four waves have the same rows and
@@ -343,10 +332,26 @@ struct KvAttn {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int key = key0 + 16 * t + 4 * g + i;
+          // a value that is not finite must not reach rows that do not see it (0
+          // times it is NaN): those that do get it through their probability
+          bool bad = false;
 #pragma unroll
-          for (int n = 0; n < kNT; ++n)
-            if (key < lo[n] || key >= hi[n]) S[t][n][i] = -INFINITY;
+          for (int gr = 0; gr < kNG; ++gr) {
+            const uint32_t w = params(t, 1, gr)[i];
+            const float mid = fmaf(__uint_as_float(w & 0xFFFF0000u), static_cast<float>(kMidCode<kBits>), bf16_f32(w));
+            const bool b = !(fabsf(mid) < INFINITY);
+            if (b) *reinterpret_cast<uint32_t*>(mine + kPAt + 64 * ((t * 2 + 1) * kNG + gr) + 16 * g + 4 * i) = 0;
+            bad |= b;
+          }
+#pragma unroll
+          for (int n = 0; n < kNT; ++n) {
+            if (key < lo[n] || key >= hi[n])
+              S[t][n][i] = -INFINITY;
+            else if (bad)
+              S[t][n][i] = __uint_as_float(0x7FC00000u);
+          }
         }
+      wave_fence();
     }
     // running maxima
     float top[kNT];
@@ -378,35 +383,29 @@ struct KvAttn {
       }
     }
     // largest steps
-    ev4u vp[kKT][kNG];
-#pragma unroll
-    for (int t = 0; t < kKT; ++t)
-#pragma unroll
-      for (int gr = 0; gr < kNG; ++gr) vp[t][gr] = params(t, 1, gr);
     float st[kNT][kNG];
 #pragma unroll
     for (int gr = 0; gr < kNG; ++gr) {
-      float x = 0.0f;
+      float x = 0.0f, y[kNT];
 #pragma unroll
-      for (int t = 0; t < kKT; ++t)
+      for (int n = 0; n < kNT; ++n) y[n] = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x = fmaxf(x, __uint_as_float(vp[t][gr][i] & 0xFFFF0000u));
+      for (int t = 0; t < kKT; ++t) {
+        const ev4u vp = params(t, 1, gr);
+        float s[4];
 #pragma unroll
-      for (int n = 0; n < kNT; ++n) st[n][gr] = x;
-    }
-    if (mask) {  // only of the keys that the row sees
-#pragma unroll
-      for (int gr = 0; gr < kNG; ++gr)
-#pragma unroll
-        for (int n = 0; n < kNT; ++n) {
-          float x = 0.0f;
-#pragma unroll
-          for (int t = 0; t < kKT; ++t)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              x = fmaxf(x, S[t][n][i] != -INFINITY ? __uint_as_float(vp[t][gr][i] & 0xFFFF0000u) : 0.0f);
-          st[n][gr] = x;
+        for (int i = 0; i < 4; ++i) {
+          s[i] = __uint_as_float(vp[i] & 0xFFFF0000u);
+          x = fmaxf(x, s[i]);
         }
+        if (mask)  // only of the keys that the row sees
+#pragma unroll
+          for (int n = 0; n < kNT; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[n] = fmaxf(y[n], S[t][n][i] != -INFINITY ? s[i] : 0.0f);
+      }
+#pragma unroll
+      for (int n = 0; n < kNT; ++n) st[n][gr] = mask ? y[n] : x;
     }
     bool grow = false;
 #pragma unroll
@@ -430,50 +429,48 @@ struct KvAttn {
           for (int c = 0; c < kCh; ++c) acc[n][gr * kCh + c] *= f;
         }
     }
-    // probabilities, and their products with steps and minima
-    uint32_t p[kPairs][kNG][kNT][4];
+    // probabilities, in the scores' place
 #pragma unroll
-    for (int t = 0; t < kKT; ++t) {
-      float pr[kNT][4];
+    for (int n = 0; n < kNT; ++n) {
+      const float neg = m[n] == -INFINITY ? 0.0f : -m[n];
 #pragma unroll
-      for (int n = 0; n < kNT; ++n) {
-        const float neg = m[n] == -INFINITY ? 0.0f : -m[n];
+      for (int t = 0; t < kKT; ++t)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          pr[n][i] = __builtin_amdgcn_exp2f(fmaf(S[t][n][i], rs[n], neg));
-          l[n] += pr[n][i];
+          S[t][n][i] = __builtin_amdgcn_exp2f(fmaf(S[t][n][i], rs[n], neg));
+          l[n] += S[t][n][i];
         }
-      }
+    }
+    // group by group: their products with steps and minima, and the outputs
 #pragma unroll
-      for (int gr = 0; gr < kNG; ++gr) {
+    for (int gr = 0; gr < kNG; ++gr) {
+      uint32_t p[kPairs][kNT][4];
+#pragma unroll
+      for (int t = 0; t < kKT; ++t) {
+        const ev4u vp = params(t, 1, gr);
         float vs[4], vl[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          vs[i] = __uint_as_float(vp[t][gr][i] & 0xFFFF0000u);
-          vl[i] = fmaf(vs[i], static_cast<float>(kMidCode<kBits>), bf16_f32(vp[t][gr][i]));
+          vs[i] = __uint_as_float(vp[i] & 0xFFFF0000u);
+          vl[i] = fmaf(vs[i], static_cast<float>(kMidCode<kBits>), bf16_f32(vp[i]));
         }
 #pragma unroll
         for (int n = 0; n < kNT; ++n) {
           float y[4];
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            // 0 times anything is 0: a hidden key's parameters may be NaN
-            y[i] = mul_zero(pr[n][i] * nrm[n][gr], vs[i]);
-            losum[n][gr] += mul_zero(pr[n][i], vl[i]);
+            y[i] = S[t][n][i] * nrm[n][gr] * vs[i];
+            losum[n][gr] = fmaf(S[t][n][i], vl[i], losum[n][gr]);
           }
-          p[t / 2][gr][n][2 * (t % 2)] = pack_f16(y[0], y[1]);
-          p[t / 2][gr][n][2 * (t % 2) + 1] = pack_f16(y[2], y[3]);
+          p[t / 2][n][2 * (t % 2)] = pack_f16(y[0], y[1]);
+          p[t / 2][n][2 * (t % 2) + 1] = pack_f16(y[2], y[3]);
         }
       }
-    }
-    // outputs
 #pragma unroll
-    for (int u = 0; u < kPairs; ++u)
+      for (int u = 0; u < kPairs; ++u) {
+        kv8h pf[kNT];
 #pragma unroll
-      for (int gr = 0; gr < kNG; ++gr) {
-            kv8h pf[kNT];
-#pragma unroll
-        for (int n = 0; n < kNT; ++n) pf[n] = frag(p[u][gr][n][0], p[u][gr][n][1], p[u][gr][n][2], p[u][gr][n][3]);
+        for (int n = 0; n < kNT; ++n) pf[n] = frag(p[u][n][0], p[u][n][1], p[u][n][2], p[u][n][3]);
         uint32_t w[4][kVP];  // key pairs (0,1) (2,3) of both tiles
 #pragma unroll
         for (int h = 0; h < 4; ++h) {
@@ -500,6 +497,7 @@ struct KvAttn {
             acc[n][gr * kCh + c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pf[n], acc[n][gr * kCh + c], 0, 0, 0);
         }
       }
+    }
   }
 
   // ---- the lane's sums over its keys become the row's, the accumulators become values
@@ -603,14 +601,18 @@ struct KvAttn {
     return (q0 + row / a.ratio) * a.Hq + h * a.ratio + row % a.ratio;
   }
 
-  __device__ void put(int64_t orow, int ch, const float* v, int count) const {
-    if (!check_store(kSiteStoreY, orow * kD + ch, count, a.T * a.Hq * kD)) return;
-    for (int j = 0; j < count; ++j) {
-      if (a.type == FGQ_F16)
-        Elem<FGQ_F16>::put(a.o, orow * kD + ch + j, v[j]);
-      else
-        Elem<FGQ_BF16>::put(a.o, orow * kD + ch + j, v[j]);
-    }
+  // kN consecutive channels of a row, as one store.
+  template <int kN, int kType>
+  __device__ void put(int64_t at, const float (&v)[kN]) const {
+    typedef uint32_t words __attribute__((ext_vector_type(kN / 2), aligned(2)));
+    if (!check_store(kSiteStoreY, at, kN, a.T * a.Hq * kD)) return;
+    uint32_t w[kN / 2];
+#pragma unroll
+    for (int j = 0; j < kN / 2; ++j)
+      w[j] = kType == FGQ_F16 ? pack_f16(v[2 * j], v[2 * j + 1]) : pack_bf16(v[2 * j], v[2 * j + 1]);
+    words x;
+    __builtin_memcpy(&x, w, sizeof(w));
+    *reinterpret_cast<words*>(static_cast<uint16_t*>(a.o) + at) = x;
   }
 
   // log sum exp of a row (natural logarithm), -inf for one that saw nothing
@@ -620,7 +622,8 @@ struct KvAttn {
   }
 
   // ---- every wave its own rows
-  __device__ void store(int rows, int row0, int64_t q0, int h) {
+  template <int kType>
+  __device__ void store_rows(int rows, int row0, int64_t q0, int h) const {
 #pragma unroll
     for (int n = 0; n < kNT; ++n) {
       const int row = row0 + 16 * n + c16;
@@ -635,21 +638,28 @@ struct KvAttn {
           float v[kCh];
 #pragma unroll
           for (int c = 0; c < kCh; ++c) v[c] = l[n] == 0.0f ? 0.0f : acc[n][gr * kCh + c][i] * inv;
-          put(orow, gr * kG + (4 * g + i) * kCh, v, kCh);
+          put<kCh, kType>(orow * kD + gr * kG + (4 * g + i) * kCh, v);
         }
     }
   }
+  __device__ void store(int rows, int row0, int64_t q0, int h) const {
+    if (a.type == FGQ_F16)
+      store_rows<FGQ_F16>(rows, row0, q0, h);
+    else
+      store_rows<FGQ_BF16>(rows, row0, q0, h);
+  }
 
-  // ---- the waves' parts of the same rows, 64 / kNT channels a round
-  // LDS: [wave][row] maxima and sums, then [wave][tile][row][16] outputs
-  static constexpr int kJoinB = 2 * kAttnWaves * kRows * 4 + kAttnWaves * (8 / kNT) * kRows * 64;
+  // ---- the waves' parts of the same rows, 128 / kNT channels a round.
+  // LDS: [wave][row] maxima, sums, factors, then [wave][tile][row][16] outputs
+  static constexpr int kTiles = 8 / kNT;  // accumulator tiles a round
+  static constexpr int kJoinB = 3 * kAttnWaves * kRows * 4 + kAttnWaves * kTiles * kRows * 64;
   static constexpr int kLdsB = kShare && kJoinB > kAttnWaves * kWaveB ? kJoinB : kAttnWaves * kWaveB;
   __device__ void join(unsigned char* lds, int split, int rows, int row0, int64_t q0, int h, int wave) {
-    constexpr int kTiles = 8 / kNT;                   // accumulator tiles a round
     constexpr int kRounds = (kD / 16 + kTiles - 1) / kTiles;
     float(*sm)[kRows] = reinterpret_cast<float(*)[kRows]>(lds);
     float(*sl)[kRows] = sm + kAttnWaves;
-    float(*so)[kTiles][kRows][16] = reinterpret_cast<float(*)[kTiles][kRows][16]>(lds + 2 * kAttnWaves * kRows * 4);
+    float* sf = sl[kAttnWaves];  // of each row: 1 / its sum, or 0 (one split: applied here)
+    float(*so)[kTiles][kRows][16] = reinterpret_cast<float(*)[kTiles][kRows][16]>(lds + 3 * kAttnWaves * kRows * 4);
     __syncthreads();  // the waves' own stages end here
     if (g == 0)
 #pragma unroll
@@ -658,33 +668,36 @@ struct KvAttn {
         sl[wave][16 * n + c16] = l[n];
       }
     __syncthreads();
-    float total[kNT], mx[kNT];
 #pragma unroll
     for (int n = 0; n < kNT; ++n) {
-      mx[n] = -INFINITY;
-      for (int w = 0; w < kAttnWaves; ++w) mx[n] = fmaxf(mx[n], sm[w][16 * n + c16]);
-      const float base = mx[n] == -INFINITY ? 0.0f : mx[n];
-      total[n] = 0.0f;
-      for (int w = 0; w < kAttnWaves; ++w) total[n] += sl[w][16 * n + c16] * exp2f(sm[w][16 * n + c16] - base);
-      const float f = exp2f(m[n] - base);
+      float mx = -INFINITY, total = 0.0f;
+#pragma unroll
+      for (int w = 0; w < kAttnWaves; ++w) mx = fmaxf(mx, sm[w][16 * n + c16]);
+      const float base = mx == -INFINITY ? 0.0f : mx;
+#pragma unroll
+      for (int w = 0; w < kAttnWaves; ++w)
+        total += sl[w][16 * n + c16] * __builtin_amdgcn_exp2f(sm[w][16 * n + c16] - base);
+      const float f = __builtin_amdgcn_exp2f(m[n] - base);
 #pragma unroll
       for (int j = 0; j < kD / 16; ++j) acc[n][j] *= f;
-    }
-    for (int n = 0; n < kNT; ++n) {
       const int row = row0 + 16 * n + c16;
-      if (wave == 0 && g == 0 && row < rows) {
-        const int64_t orow = out_row(q0, h, row);
-        if (a.splits == 1) {
-          put_lse(orow, mx[n], total[n]);
-        } else if (check_store(kSiteStorePart, (orow * a.splits + split) * (kD + 2) + kD, 2,
-                               a.T * a.Hq * a.splits * (kD + 2))) {
-          a.part[(orow * a.splits + split) * (kD + 2) + kD] = mx[n];
-          a.part[(orow * a.splits + split) * (kD + 2) + kD + 1] = total[n];
+      if (wave == 0 && g == 0) {
+        sf[16 * n + c16] = total == 0.0f ? 0.0f : 1.0f / total;
+        if (row < rows) {
+          const int64_t orow = out_row(q0, h, row);
+          if (a.splits == 1) {
+            put_lse(orow, mx, total);
+          } else if (check_store(kSiteStorePart, (orow * a.splits + split) * (kD + 2) + kD, 2,
+                                 a.T * a.Hq * a.splits * (kD + 2))) {
+            a.part[(orow * a.splits + split) * (kD + 2) + kD] = mx;
+            a.part[(orow * a.splits + split) * (kD + 2) + kD + 1] = total;
+          }
         }
       }
     }
 #pragma unroll
     for (int rd = 0; rd < kRounds; ++rd) {
+      if (rd > 0) __syncthreads();
 #pragma unroll
       for (int n = 0; n < kNT; ++n)
 #pragma unroll
@@ -692,51 +705,66 @@ struct KvAttn {
           if (rd * kTiles + j < kD / 16)
             *reinterpret_cast<kv4f*>(&so[wave][j][16 * n + c16][4 * g]) = acc[n][(rd * kTiles + j) % (kD / 16)];
       __syncthreads();
-      for (int e = threadIdx.x; e < kTiles * kRows * 16; e += kAttnThreads) {
-        const int i = e % 16, rr = e / 16 % kRows, j = e / 16 / kRows, ti = rd * kTiles + j;
+      // a thread takes a row's kN neighbouring channels: kN tiles of one group at one of 16
+      constexpr int kN = kCh < kTiles ? kCh : kTiles;
+      for (int e = threadIdx.x; e < kTiles / kN * kRows * 16; e += kAttnThreads) {
+        const int i = e % 16, rr = e / 16 % kRows, j = e / 16 / kRows * kN, ti = rd * kTiles + j;
         const int row = row0 + rr;
         if (ti >= kD / 16 || row >= rows) continue;
-        float v = 0.0f, sum = 0.0f;
-        float mm = -INFINITY;
-        for (int w = 0; w < kAttnWaves; ++w) mm = fmaxf(mm, sm[w][rr]);
-        const float base = mm == -INFINITY ? 0.0f : mm;
-        for (int w = 0; w < kAttnWaves; ++w) {
-          v += so[w][j][rr][i];
-          sum += sl[w][rr] * exp2f(sm[w][rr] - base);
+        float v[kN];
+#pragma unroll
+        for (int c = 0; c < kN; ++c) {
+          v[c] = so[0][j + c][rr][i];
+#pragma unroll
+          for (int w = 1; w < kAttnWaves; ++w) v[c] += so[w][j + c][rr][i];
         }
         const int ch = ti / kCh * kG + i * kCh + ti % kCh;
         const int64_t orow = out_row(q0, h, row);
         if (a.splits == 1) {
-          v = sum == 0.0f ? 0.0f : v / sum;
-          put(orow, ch, &v, 1);
-        } else if (check_store(kSiteStorePart, (orow * a.splits + split) * (kD + 2) + ch, 1,
+#pragma unroll
+          for (int c = 0; c < kN; ++c) v[c] = sf[rr] == 0.0f ? 0.0f : v[c] * sf[rr];
+          if (a.type == FGQ_F16)
+            put<kN, FGQ_F16>(orow * kD + ch, v);
+          else
+            put<kN, FGQ_BF16>(orow * kD + ch, v);
+        } else if (check_store(kSiteStorePart, (orow * a.splits + split) * (kD + 2) + ch, kN,
                                a.T * a.Hq * a.splits * (kD + 2))) {
-          a.part[(orow * a.splits + split) * (kD + 2) + ch] = v;
+#pragma unroll
+          for (int c = 0; c < kN; ++c) a.part[(orow * a.splits + split) * (kD + 2) + ch + c] = v[c];
         }
       }
-      __syncthreads();
     }
   }
 };
 
+// Waves a SIMD that the registers have to allow: few rows are bound by memory
+// and want three (168 registers), large heads and many groups would spill at two.
+template <int kD, int kG, int kNT>
+constexpr int kMinWaves = kD == 256 || (kD / kG) * kNT >= 8 ? 1 : kNT == 1 && kD / kG <= 2 ? 3 : 2;
+
 template <int kBits, int kD, int kG, int kNT, bool kShare, int kKT>
-__global__ __launch_bounds__(kAttnThreads, LB) void kv_attn_kernel(KvAttnArgs a) {
+__global__ __launch_bounds__(kAttnThreads, (kMinWaves<kD, kG, kNT>)) void kv_attn_kernel(KvAttnArgs a) {
   typedef KvAttn<kBits, kD, kG, kNT, kShare, kKT> K;
   __shared__ __attribute__((aligned(16))) unsigned char lds[K::kLdsB];
   K k(a);
   k.run(lds);
 }
 
+template <int kBits, int kD, int kG, int kNT, bool kShare>
+void launch_nt(const KvAttnArgs& a, hipStream_t st) {
+  constexpr int kKT = kD * kBits <= 512 && kD == kG ? 4 : 2;
+  const dim3 grid(static_cast<uint32_t>(static_cast<int64_t>(a.B) * a.Hkv * a.tiles * a.splits));
+  hipLaunchKernelGGL((kv_attn_kernel<kBits, kD, kG, kNT, kShare, kKT>), grid, dim3(kAttnThreads), 0, st, a);
+}
+
 template <int kBits, int kD, int kG>
 fgq_status launch_one(const KvAttnArgs& a, int nt, bool share, hipStream_t st) {
-  constexpr int kKT = kD * kBits <= 512 && kD == kG ? 4 : 2;
-  const dim3 grid(static_cast<uint32_t>(static_cast<int64_t>(a.B) * a.Hkv * a.tiles * a.splits)), wg(kAttnThreads);
   if (share && nt == 1)
-    hipLaunchKernelGGL((kv_attn_kernel<kBits, kD, kG, 1, true, kKT>), grid, wg, 0, st, a);
+    launch_nt<kBits, kD, kG, 1, true>(a, st);
   else if (share)
-    hipLaunchKernelGGL((kv_attn_kernel<kBits, kD, kG, 2, true, kKT>), grid, wg, 0, st, a);
+    launch_nt<kBits, kD, kG, 2, true>(a, st);
   else
-    hipLaunchKernelGGL((kv_attn_kernel<kBits, kD, kG, 2, false, kKT>), grid, wg, 0, st, a);
+    launch_nt<kBits, kD, kG, 2, false>(a, st);
   return last_launch();
 }
 
