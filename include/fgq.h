@@ -602,7 +602,7 @@ fgq_status fgq_quantize_rows(const void* x, int32_t x_type, int64_t M,
  * fgq_linear_i8 -- the same on floating-point rows: y = fgq_gemm_i8 of
  * fgq_quantize_rows(x), value for value.
  *   ws  [tmp] device buffer of fgq_linear_i8_ws_bytes(M, K, O) bytes, 16-byte
- *             aligned, not kept between calls
+ *             aligned, not kept between calls; may be NULL when that is 0
  */
 fgq_status fgq_gemm_i8(const int8_t* q, int64_t ldq, const float* sx, int64_t M,
                        int64_t K, const int8_t* w, int64_t ldw, const float* sw,

@@ -31,6 +31,11 @@ fgq_status check_cache(int64_t num_pages, int32_t Hkv, int32_t D, int32_t P, int
   return FGQ_OK;
 }
 
+// Whether fgq_linear_i8 quantizes the rows in the product itself.
+bool linear_fused(int64_t M, int64_t K) {
+  return M <= kI8FusedRows && M * (round_up(K, kI8RowStep) + 16) <= kI8FusedBytes;
+}
+
 bool kv_grid_ok(int64_t T, const KvGeom& c) { return T <= (1LL << 38) / (static_cast<int64_t>(c.Hkv) * c.D / 8); }
 
 }  // namespace
@@ -62,7 +67,7 @@ fgq_status fgq_gemm_i8(const int8_t* q, int64_t ldq, const float* sx, int64_t M,
 }
 
 size_t fgq_linear_i8_ws_bytes(int64_t M, int64_t K, int64_t O) {
-  if (M < 1 || K < 1 || O < 1) return 0;
+  if (M < 1 || K < 1 || O < 1 || linear_fused(M, K)) return 0;
   return static_cast<size_t>(M) * (round_up(K, kI8RowStep) + 4);
 }
 
@@ -74,13 +79,13 @@ fgq_status fgq_linear_i8(const void* x, int32_t x_type, int64_t ldx, int64_t M, 
   if (ldx < K || !type_ok(x_type) || !aligned(x, type_bytes(x_type))) return FGQ_ERR_SHAPE;
   if (M == 0) return FGQ_OK;
   if (!x || !w || !sw || !y) return FGQ_ERR_NULL;
-  if (!ws || !aligned(ws, 16) || ws_bytes < fgq_linear_i8_ws_bytes(M, K, O)) return FGQ_ERR_WORKSPACE;
   const int64_t ldq = round_up(K, kI8RowStep);
-  if (M <= kI8FusedRows && M * (ldq + 16) <= kI8FusedBytes) {
+  if (linear_fused(M, K)) {
     const i8::I8Args a{nullptr, w, nullptr, sw, bias, y, 0, ldw, ldy, static_cast<int32_t>(M), static_cast<int32_t>(O),
                        static_cast<int32_t>(ceil_div(K, kI8RowStep))};
     return launch_i8_fused(x, x_type, ldx, K, a, y_type, as_stream(stream));
   }
+  if (!ws || !aligned(ws, 16) || ws_bytes < fgq_linear_i8_ws_bytes(M, K, O)) return FGQ_ERR_WORKSPACE;
   int8_t* q = static_cast<int8_t*>(ws);
   float* sx = reinterpret_cast<float*>(q + M * ldq);
   rc = launch_quantize_rows(x, x_type, M, K, ldx, q, ldq, sx, as_stream(stream));

@@ -562,6 +562,11 @@ struct KvAttn {
       k0 += split * a.split_keys;
       k1 = min(k1, k0 + a.split_keys);
     }
+    const int first = k0 + (kShare ? wave * kKeys : 0), hop = kShare ? kAttnWaves * kKeys : kKeys;
+    const int last = k1 - 1;
+    // the first step's bytes are on their way while the queries are prepared
+    Raw r;
+    if (first < k1) load(r, first, last);
 #pragma unroll
     for (int t = 0; t < kNT; ++t) {
       const int row = min(row0 + 16 * t + c16, rl);
@@ -579,10 +584,6 @@ struct KvAttn {
 #pragma unroll
       for (int j = 0; j < kD / 16; ++j) acc[t][j] = kv4f{0, 0, 0, 0};
     }
-    const int first = k0 + (kShare ? wave * kKeys : 0), hop = kShare ? kAttnWaves * kKeys : kKeys;
-    const int last = k1 - 1;
-    Raw r;
-    if (first < k1) load(r, first, last);
     for (int key = first; key < k1; key += hop) {
       stage(r);
       if (key + hop < k1) load(r, key + hop, last);

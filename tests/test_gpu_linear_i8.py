@@ -186,7 +186,7 @@ def test_refusals():
             (lambda: fgq.fgq_linear_i8(xd, wq.float(), sw), TypeError),
             (lambda: fgq.fgq_linear_i8(xd, wq, sw, bias=sw[:3]), ValueError),
             (lambda: fgq.fgq_linear_i8(xd, wq, sw, y=torch.empty(4, 9, device="cuda")), ValueError),
-            (lambda: fgq.fgq_linear_i8(xd, wq, sw, ws=torch.empty(16, dtype=torch.uint8, device="cuda")),
+            (lambda: fgq.fgq_linear_i8(xd.repeat(10, 1), wq, sw, ws=torch.empty(16, dtype=torch.uint8, device="cuda")),
              fgq.FgqError),
             (lambda: fgq.fgq_gemm_i8(wq, sw, 200, wq, sw), ValueError)]:
         with pytest.raises(err):
