@@ -36,7 +36,8 @@ bool linear_fused(int64_t M, int64_t K) {
   return M <= kI8FusedRows && M * (round_up(K, kI8RowStep) + 16) <= kI8FusedBytes;
 }
 
-bool kv_grid_ok(int64_t T, const KvGeom& c) { return T <= (1LL << 38) / (static_cast<int64_t>(c.Hkv) * c.D / 8); }
+// Workgroups of the cache's kernels: tokens in 31 bits, parts of a token in 16.
+bool kv_grid_ok(int64_t T, const KvGeom& c) { return T < (1LL << 31) && static_cast<int64_t>(c.Hkv) * c.D <= (1LL << 26); }
 
 }  // namespace
 

@@ -3,20 +3,25 @@
 //
 // A lane holds eight consecutive channels, so a group of G channels is G / 8
 // neighbouring lanes that agree on its minimum and maximum by exchanges within
-// the wave; one pass over the data, bound by its bytes.
+// a row of 16 lanes; one pass over the data, kTokens tokens of a thread in
+// flight.  The threads of a workgroup are the eights of a token's heads,
+// several tokens' where those are few, so that the divisions are made once a
+// thread.
 //
 // lo is the minimum rounded down to bf16 and step the range over the number of
 // steps rounded up to bf16 (to bf16 because the exponent range of every input
 // type has to fit): every value then lies within [lo, lo + L * step], so it is
 // at most half a step from the value its code stands for.
+#include <type_traits>
+
 #include "elem.h"
 #include "kvcache.h"
-#include "rowquant.h"
 
 namespace fgq {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kTokens = 4;
 
 struct KvArgs {
   const void* src[2];
@@ -24,111 +29,166 @@ struct KvArgs {
   int64_t st[2], sh[2];  // strides of src in elements: token, head
   const int64_t* slots;
   uint8_t* cache;
-  int64_t T, num_slots, items;
-  int32_t Hkv, D, P, G, row, ng;
+  int64_t T, num_slots;
+  int32_t Hkv, D, P, G, row, ng, pshift, gshift;
+  int32_t per;  // tokens a workgroup has at a time (1: a part of one, blockIdx.y)
   int64_t head_bytes;
 };
 
-// Which eight channels this thread has: token, head, eighth of the head.
+// Which channels a thread has: head, eighth of the head, and of its
+// workgroup's tokens the first.
 struct Item {
   int64_t t;
   int h, d8;
+  bool have;
 };
-__device__ inline Item item_of(const KvArgs& a, int64_t i) {
-  const int n8 = a.D / 8;
-  const int64_t th = i / n8;
-  return Item{th / a.Hkv, static_cast<int>(th % a.Hkv), static_cast<int>(i % n8)};
+__device__ inline Item item_of(const KvArgs& a) {
+  const uint32_t n8 = a.D / 8, n = a.Hkv * n8;
+  uint32_t col = threadIdx.x, local = 0;
+  if (a.per > 1) {
+    local = col / n;
+    col -= local * n;
+  } else {
+    col += blockIdx.y * kThreads;
+  }
+  const uint32_t h = col / n8;
+  return Item{static_cast<int64_t>(blockIdx.x) * a.per * kTokens + local, static_cast<int>(h),
+              static_cast<int>(col - h * n8), a.per > 1 ? local < static_cast<uint32_t>(a.per) : col < n};
+}
+
+// The other lanes' value at distance 1, 2 (exchanges within four lanes), 4 and 8
+// (mirrors of 8 and 16, whose quarters agree by then).
+template <int kStep>
+__device__ inline float other(float v) {
+  constexpr int kCtrl = kStep == 1 ? 0xB1 : kStep == 2 ? 0x4E : kStep == 4 ? 0x141 : 0x140;
+  return __uint_as_float(static_cast<uint32_t>(
+      __builtin_amdgcn_update_dpp(0, static_cast<int>(__float_as_uint(v)), kCtrl, 0xF, 0xF, true)));
+}
+template <int kStep>
+__device__ inline void meet(float& lo, float& hi, float& bad) {
+  lo = fminf(lo, other<kStep>(lo));
+  hi = fmaxf(hi, other<kStep>(hi));
+  bad += other<kStep>(bad);
 }
 
 template <int kType, int kBits>
 __global__ __launch_bounds__(kThreads) void kv_write_kernel(KvArgs a) {
 #pragma clang fp contract(off)
   constexpr float L = kBits == 4 ? 15.0f : 255.0f;
-  const int z = blockIdx.y;  // 0: keys, 1: values
-  const int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
-  const bool have = i < a.items;
-  const Item it = item_of(a, have ? i : 0);
-  const int64_t slot = have ? a.slots[it.t] : -1;
-  float v[8];
-  values8<kType>(load8<kType>(a.src[z], it.t * a.st[z] + it.h * a.sh[z] + 8 * it.d8), v);
-  float lo = v[0], hi = v[0];
-  uint32_t big = 0;
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    lo = fminf(lo, v[j]);
-    hi = fmaxf(hi, v[j]);
-    big = max(big, abs_bits(v[j]));
-  }
-  const int lanes = a.G / 8;  // 4, 8 or 16: whole groups in every wave
-  for (int off = 1; off < lanes; off *= 2) {
-    lo = fminf(lo, __shfl_xor(lo, off));
-    hi = fmaxf(hi, __shfl_xor(hi, off));
-    big = max(big, static_cast<uint32_t>(__shfl_xor(static_cast<int>(big), off)));
-  }
-  uint32_t u = __float_as_uint(lo);
-  u = (static_cast<int32_t>(u) < 0 ? u + 0xFFFFu : u) & 0xFFFF0000u;
-  lo = __uint_as_float(u);
-  const float s = (hi * 0.5f - lo * 0.5f) * (2.0f / L);
-  uint32_t t = (__float_as_uint(s) + 0xFFFFu) & 0xFFFF0000u;
-  if (__uint_as_float(t) < 0x1p-120f) t = 0;
-  float inv = t ? 1.0f / __uint_as_float(t) : 0.0f;
-  if (big >= 0x7F800000u || u == 0xFF800000u) {  // not finite (or lo is not, in bf16): the group reads back NaN
-    u = t = 0x7FC00000u;
-    inv = 0.0f;
-  }
-  uint32_t c[8];
-#pragma unroll
-  for (int j = 0; j < 8; ++j) c[j] = static_cast<uint32_t>(fminf(fmaxf(rintf((v[j] - lo) * inv), 0.0f), L));
-  if (slot < 0 || slot >= a.num_slots) return;
-  const int64_t page = slot / a.P;
-  const int at = static_cast<int>(slot % a.P);
-  const int64_t base = (page * a.Hkv + it.h) * a.head_bytes;
+  const int z = blockIdx.z;  // 0: keys, 1: values
+  const Item it = item_of(a);
   const int64_t limit = a.num_slots / a.P * a.Hkv * a.head_bytes;
-  const int64_t cd = base + static_cast<int64_t>(z * a.P + at) * a.row + it.d8 * kBits;
-  if (check_store(kSiteStoreCache, cd, kBits, limit)) {
-    if constexpr (kBits == 4) {
-      uint32_t w = 0;
+  Raw8<kType> raw[kTokens];
+  int64_t slot[kTokens];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) w |= c[j] << (4 * j);
-      *reinterpret_cast<uint32_t*>(a.cache + cd) = w;
-    } else {
-      uint64_t w = 0;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) w |= static_cast<uint64_t>(c[j]) << (8 * j);
-      *reinterpret_cast<uint64_t*>(a.cache + cd) = w;
-    }
+  for (int u = 0; u < kTokens; ++u) {
+    const int64_t t = it.t + u * a.per;
+    const bool have = it.have && t < a.T;
+    slot[u] = have ? a.slots[t] : -1;
+    raw[u] = load8<kType>(a.src[z], have ? t * a.st[z] + it.h * a.sh[z] + 8 * it.d8 : 0);
   }
-  if (it.d8 % lanes == 0) {
-    const int64_t pp = base + 2LL * a.P * a.row + 4LL * ((z * a.ng + it.d8 / lanes) * a.P + at);
-    if (check_store(kSiteStoreCache, pp, 4, limit)) *reinterpret_cast<uint32_t*>(a.cache + pp) = u >> 16 | t;
+#pragma unroll
+  for (int u = 0; u < kTokens; ++u) {
+    float v[8];
+    values8<kType>(raw[u], v);
+    float lo = v[0], hi = v[0], bad = 0.0f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      lo = fminf(lo, v[j]);
+      hi = fmaxf(hi, v[j]);
+      bad = __builtin_fmaf(v[j], 0.0f, bad);  // NaN if any value is not finite
+    }
+    meet<1>(lo, hi, bad);
+    meet<2>(lo, hi, bad);
+    if (a.G > 32) meet<4>(lo, hi, bad);
+    if (a.G > 64) meet<8>(lo, hi, bad);
+    uint32_t w = __float_as_uint(lo);
+    w = (static_cast<int32_t>(w) < 0 ? w + 0xFFFFu : w) & 0xFFFF0000u;
+    lo = __uint_as_float(w);
+    const float s = (hi * 0.5f - lo * 0.5f) * (2.0f / L);
+    uint32_t t = (__float_as_uint(s) + 0xFFFFu) & 0xFFFF0000u;
+    if (__uint_as_float(t) < 0x1p-120f) t = 0;
+    float inv = t ? 1.0f / __uint_as_float(t) : 0.0f;
+    if (bad != 0.0f || w == 0xFF800000u) {  // not finite (or lo is not, in bf16): the group reads back NaN
+      w = t = 0x7FC00000u;
+      inv = 0.0f;
+    }
+    // Adding 1.5 * 2^23 rounds to even at the unit and leaves the code in the low
+    // byte; x >= lo, and the quotient passes L only where the range overflows.
+    uint32_t c[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) c[j] = __float_as_uint(fminf((v[j] - lo) * inv, L) + 12582912.0f);
+    if (slot[u] < 0 || slot[u] >= a.num_slots) continue;
+    const int64_t page = slot[u] >> a.pshift;
+    const int at = static_cast<int>(slot[u]) & (a.P - 1);
+    const int64_t base = (page * a.Hkv + it.h) * a.head_bytes;
+    const int64_t cd = base + static_cast<int64_t>(z * a.P + at) * a.row + it.d8 * kBits;
+    // bytes of four codes
+    auto four = [](uint32_t b0, uint32_t b1, uint32_t b2, uint32_t b3) {
+      return __builtin_amdgcn_perm(b1, b0, 0x0C0C0400u) | __builtin_amdgcn_perm(b3, b2, 0x04000C0Cu);
+    };
+    if (check_store(kSiteStoreCache, cd, kBits, limit)) {
+      if constexpr (kBits == 4) {
+        const uint32_t q = four(c[0], c[2], c[4], c[6]) | four(c[1], c[3], c[5], c[7]) << 4;
+        *reinterpret_cast<uint32_t*>(a.cache + cd) = inv > 0.0f ? q : 0;
+      } else {
+        const uint64_t q = static_cast<uint64_t>(four(c[4], c[5], c[6], c[7])) << 32 | four(c[0], c[1], c[2], c[3]);
+        *reinterpret_cast<uint64_t*>(a.cache + cd) = inv > 0.0f ? q : 0;
+      }
+    }
+    if ((8 * it.d8 & (a.G - 1)) == 0) {
+      const int64_t pp = base + 2LL * a.P * a.row + 4LL * ((z * a.ng + (8 * it.d8 >> a.gshift)) * a.P + at);
+      if (check_store(kSiteStoreCache, pp, 4, limit)) *reinterpret_cast<uint32_t*>(a.cache + pp) = w >> 16 | t;
+    }
   }
 }
 
 template <int kType, int kBits>
 __global__ __launch_bounds__(kThreads) void kv_read_kernel(KvArgs a) {
-  const int z = blockIdx.y;
-  const int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
-  if (i >= a.items) return;
-  const Item it = item_of(a, i);
-  const int64_t slot = a.slots[it.t];
-  float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-  if (slot >= 0 && slot < a.num_slots) {
-    const int64_t page = slot / a.P;
-    const int at = static_cast<int>(slot % a.P);
-    const uint8_t* base = a.cache + (page * a.Hkv + it.h) * a.head_bytes;
-    const uint8_t* cd = base + static_cast<int64_t>(z * a.P + at) * a.row + it.d8 * kBits;
-    const uint32_t par = *reinterpret_cast<const uint32_t*>(
-        base + 2LL * a.P * a.row + 4LL * ((z * a.ng + 8 * it.d8 / a.G) * a.P + at));
-    const float lo = bf16_f32(par & 0xFFFFu), step = __uint_as_float(par & 0xFFFF0000u);
-    uint64_t w;
-    if constexpr (kBits == 4)
-      w = *reinterpret_cast<const uint32_t*>(cd);
-    else
-      w = *reinterpret_cast<const uint64_t*>(cd);
+  const int z = blockIdx.z;
+  const Item it = item_of(a);
+  if (!it.have) return;
+  int64_t slot[kTokens];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = fmaf(step, static_cast<float>(w >> (kBits * j) & ((1 << kBits) - 1)), lo);
+  for (int u = 0; u < kTokens; ++u) {
+    const int64_t t = it.t + u * a.per;
+    slot[u] = t < a.T ? a.slots[t] : -1;
   }
-  if (check_store(kSiteStoreY, 8 * i, 8, 8 * a.items)) store8<kType>(a.dst[z], 8 * i, v);
+  typedef typename std::conditional<kBits == 4, uint32_t, uint2>::type codes;
+  codes w[kTokens] = {};
+  uint32_t par[kTokens] = {};  // 0: the value 0
+#pragma unroll
+  for (int u = 0; u < kTokens; ++u)
+    if (slot[u] >= 0 && slot[u] < a.num_slots) {
+      const int64_t page = slot[u] >> a.pshift;
+      const int at = static_cast<int>(slot[u]) & (a.P - 1);
+      const uint8_t* base = a.cache + (page * a.Hkv + it.h) * a.head_bytes;
+      w[u] = *reinterpret_cast<const codes*>(base + static_cast<int64_t>(z * a.P + at) * a.row + it.d8 * kBits);
+      par[u] = *reinterpret_cast<const uint32_t*>(
+          base + 2LL * a.P * a.row + 4LL * ((z * a.ng + (8 * it.d8 >> a.gshift)) * a.P + at));
+    }
+#pragma unroll
+  for (int u = 0; u < kTokens; ++u) {
+    const int64_t t = it.t + u * a.per;
+    if (t >= a.T) break;
+    const float lo = bf16_f32(par[u] & 0xFFFFu), step = __uint_as_float(par[u] & 0xFFFF0000u);
+    uint32_t even, odd;  // bytes of codes: 4 bits 0 2 4 6 and 1 3 5 7, 8 bits 0 1 2 3 and 4 5 6 7
+    if constexpr (kBits == 4) {
+      even = w[u] & 0x0F0F0F0Fu;
+      odd = w[u] >> 4 & 0x0F0F0F0Fu;
+    } else {
+      even = w[u].x;
+      odd = w[u].y;
+    }
+    float v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const uint32_t b = kBits == 4 ? (j % 2 ? odd : even) >> (8 * (j / 2)) : (j < 4 ? even : odd) >> (8 * (j % 4));
+      v[j] = fmaf(step, static_cast<float>(b & 0xFFu), lo);
+    }
+    const int64_t to = (t * a.Hkv + it.h) * a.D + 8 * it.d8;
+    if (check_store(kSiteStoreY, to, 8, a.T * a.Hkv * a.D)) store8<kType>(a.dst[z], to, v);
+  }
 }
 
 KvArgs kv_args(const KvGeom& c, int64_t T, const int64_t* slots) {
@@ -136,7 +196,10 @@ KvArgs kv_args(const KvGeom& c, int64_t T, const int64_t* slots) {
   a.slots = slots;
   a.T = T;
   a.num_slots = c.num_pages * c.P;
-  a.items = T * c.Hkv * (c.D / 8);
+  a.pshift = __builtin_ctz(c.P);
+  a.gshift = __builtin_ctz(c.G);
+  const int32_t n = c.Hkv * (c.D / 8);
+  a.per = n <= kThreads / 2 ? kThreads / n : 1;
   a.Hkv = c.Hkv;
   a.D = c.D;
   a.P = c.P;
@@ -145,6 +208,12 @@ KvArgs kv_args(const KvGeom& c, int64_t T, const int64_t* slots) {
   a.ng = c.D / c.G;
   a.head_bytes = kv_head_bytes(c.P, c.D, c.bits, c.G);
   return a;
+}
+
+dim3 kv_grid(const KvArgs& a) {
+  const int32_t n = a.Hkv * (a.D / 8);
+  return dim3(static_cast<uint32_t>(ceil_div(a.T, static_cast<int64_t>(a.per) * kTokens)),
+              a.per > 1 ? 1 : static_cast<uint32_t>(ceil_div(n, kThreads)), 2);
 }
 
 }  // namespace
@@ -159,7 +228,7 @@ fgq_status launch_kv_write(const void* k, const void* v, int32_t type, int64_t T
   a.st[1] = stride[2];
   a.sh[1] = stride[3];
   a.cache = cache;
-  const dim3 grid(static_cast<uint32_t>(ceil_div(a.items, kThreads)), 2);
+  const dim3 grid = kv_grid(a);
   return with_type(type, [&](auto t) {
     if (c.bits == 4)
       hipLaunchKernelGGL((kv_write_kernel<decltype(t)::value, 4>), grid, dim3(kThreads), 0, st, a);
@@ -175,7 +244,7 @@ fgq_status launch_kv_read(const int64_t* slots, int64_t T, const KvGeom& c, cons
   a.dst[0] = k;
   a.dst[1] = v;
   a.cache = const_cast<uint8_t*>(cache);
-  const dim3 grid(static_cast<uint32_t>(ceil_div(a.items, kThreads)), 2);
+  const dim3 grid = kv_grid(a);
   return with_type(type, [&](auto t) {
     if (c.bits == 4)
       hipLaunchKernelGGL((kv_read_kernel<decltype(t)::value, 4>), grid, dim3(kThreads), 0, st, a);
