@@ -23,10 +23,11 @@ fgq_status check_i8(int64_t M, int64_t K, int64_t O, int64_t ldw, int64_t ldy, i
 
 fgq_status check_cache(int64_t num_pages, int32_t Hkv, int32_t D, int32_t P, int32_t bits, int32_t G, KvGeom* c) {
   if (bits != 4 && bits != 8) return FGQ_ERR_BITS;
-  if (num_pages < 1 || Hkv < 1 || D < 1 || P < 1 || num_pages >= (1LL << 31) || D > (1 << 16) || Hkv > (1 << 16))
+  if (num_pages < 1 || Hkv < 1 || D < 1 || P < 1 || num_pages >= (1LL << 31) || Hkv > (1 << 16))
     return FGQ_ERR_SHAPE;
   if ((G != 32 && G != 64 && G != 128) || D % G != 0) return FGQ_ERR_GROUP;
-  if (P < 16 || P > 1024 || (P & (P - 1)) != 0) return FGQ_ERR_UNSUPPORTED;
+  if (D > 2048 || P < 16 || P > 1024 || (P & (P - 1)) != 0) return FGQ_ERR_UNSUPPORTED;
+  if (Hkv * kv_head_bytes(P, D, bits, G) >= (1LL << 31)) return FGQ_ERR_UNSUPPORTED;  // 32-bit offsets in a page
   *c = KvGeom{num_pages, Hkv, D, P, bits, G};
   return FGQ_OK;
 }
@@ -36,8 +37,8 @@ bool linear_fused(int64_t M, int64_t K) {
   return M <= kI8FusedRows && M * (round_up(K, kI8RowStep) + 16) <= kI8FusedBytes;
 }
 
-// Workgroups of the cache's kernels: tokens in 31 bits, parts of a token in 16.
-bool kv_grid_ok(int64_t T, const KvGeom& c) { return T < (1LL << 31) && static_cast<int64_t>(c.Hkv) * c.D <= (1LL << 26); }
+// Workgroups of the cache's kernels: tokens in 31 bits, heads in 16.
+bool kv_grid_ok(int64_t T, const KvGeom& c) { return T < (1LL << 31) && c.Hkv < (1 << 16); }
 
 }  // namespace
 

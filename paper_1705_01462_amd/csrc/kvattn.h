@@ -12,6 +12,9 @@ namespace fgq {
 // most kKvAttnAlign keys, are whole in it).
 constexpr int kKvAttnAlign = 64, kKvAttnSplit = 256;
 
+// Whether there is a form with eight waves a workgroup (their registers allow it).
+inline bool kv_attn_has_wide(int32_t D, int32_t G) { return D < 256 && D / G <= 2; }
+
 struct KvAttnArgs {
   const void* q;           // [T][Hq][D], strides in elements
   int64_t q_st, q_sh;
@@ -29,6 +32,7 @@ struct KvAttnArgs {
   float scale_log2;        // softmax scale * log2 e
   int32_t tiles;           // row tiles a key head (of max_q queries)
   int32_t splits, split_keys;
+  int32_t wide;            // eight waves a workgroup instead of four (share)
 };
 
 // One launch for a head size (kvattn_d*.hip); nt: 16-row blocks a wave;

@@ -90,7 +90,7 @@ void launch_join(const KvAttnArgs& a, int64_t items, hipStream_t st) {
 
 struct Plan {
   int nt, tiles, splits, split_keys;
-  bool share;
+  bool share, wide;
 };
 
 // max_keys: the most keys of a sequence, as far as the host knows.  Three
@@ -98,7 +98,7 @@ struct Plan {
 // sequences of 131072 keys and 16 (sequence, key head) pairs: 1.5 a unit 89, 3
 // 72, 6 80, 12 89; 48 sequences of up to 8191: 90, 82, 91, 99), but not below
 // 512 keys, which four waves step through a few times.
-Plan plan(int32_t Hq, int32_t Hkv, int64_t B, int64_t max_q, int64_t max_keys, int64_t window) {
+Plan plan(int32_t D, int32_t G, int32_t Hq, int32_t Hkv, int64_t B, int64_t max_q, int64_t max_keys, int64_t window) {
   Plan p{};
   const int64_t rows = max_q * (Hq / Hkv);
   p.share = rows <= 64;
@@ -108,8 +108,15 @@ Plan plan(int32_t Hq, int32_t Hkv, int64_t B, int64_t max_q, int64_t max_keys, i
   const int64_t keys = (window ? std::min(max_keys, window + max_q) : max_keys) + kKvAttnAlign;
   p.splits = 1;
   if (p.share) {
-    const int64_t wgs = B * Hkv * p.tiles, want = 3LL * ig::device_cus();
-    p.splits = static_cast<int>(std::max<int64_t>(1, std::min({keys / kKvAttnSplit, want / wgs, int64_t{1024}})));
+    const int64_t wgs = B * Hkv * p.tiles, cus = ig::device_cus();
+    p.splits = static_cast<int>(std::max<int64_t>(1, std::min({keys / kKvAttnSplit, 3 * cus / wgs, int64_t{1024}})));
+    // Some hundred keys and few workgroups: eight waves take them without a join
+    // (us: 8 pairs of 777 keys 12.5 instead of 13.9, 192 pairs of a window of 512
+    // 12.3 instead of 17.4; 64 pairs of 4096 keys 36 instead of 22.5).
+    if (kv_attn_has_wide(D, G) && wgs <= cus && keys > 256 && keys <= 1024) {
+      p.wide = true;
+      p.splits = 1;
+    }
   }
   p.split_keys = static_cast<int>(round_up(ceil_div(keys, p.splits), kKvAttnSplit));
   p.splits = static_cast<int>(ceil_div(keys, p.split_keys));
@@ -119,14 +126,16 @@ Plan plan(int32_t Hq, int32_t Hkv, int64_t B, int64_t max_q, int64_t max_keys, i
 }  // namespace
 
 size_t kv_attn_ws_bytes(int64_t T, int32_t Hq, int32_t Hkv, int32_t D, int64_t B, int64_t max_q, int64_t max_keys) {
-  const Plan p = plan(Hq, Hkv, B, max_q, max_keys, 0);
+  // without a group size and a window: at least as many splits as with them
+  const Plan p = plan(256, 32, Hq, Hkv, B, max_q, max_keys, 0);
   return p.splits == 1 ? 0 : static_cast<size_t>(T) * Hq * p.splits * (D + 2) * sizeof(float);
 }
 
 fgq_status launch_kv_attn(KvAttnArgs a, void* ws, hipStream_t st) {
-  const Plan p = plan(a.Hq, a.Hkv, a.B, a.max_q, a.max_pages * a.P, a.window);
+  const Plan p = plan(a.D, a.G, a.Hq, a.Hkv, a.B, a.max_q, a.max_pages * a.P, a.window);
   a.tiles = p.tiles;
   a.splits = p.splits;
+  a.wide = p.wide ? 1 : 0;
   a.split_keys = p.split_keys;
   a.part = static_cast<float*>(ws);
   const fgq_status rc = a.D == 64    ? launch_kv_attn_d64(a, p.nt, p.share, st)

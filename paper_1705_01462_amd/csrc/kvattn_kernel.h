@@ -46,8 +46,6 @@ typedef float kv4f __attribute__((ext_vector_type(4)));
 
 constexpr float kSlack = 4.0f;     // log2 of how far a score may pass its row's maximum
 constexpr float kBoost = 2048.0f;  // 2^11: the largest rounded probability is 2^(4 + 11)
-constexpr int kAttnThreads = 256;
-constexpr int kAttnWaves = 4;
 #ifndef KT
 #define KT 2
 #endif
@@ -94,10 +92,10 @@ __device__ inline uint32_t value_pair(uint32_t w, int n) {
   return __builtin_bit_cast(uint32_t, __builtin_bit_cast(v2h, c) + __builtin_bit_cast(v2h, mid));
 }
 
-// kNT: 16-row blocks a wave.  kShare: the four waves have the same rows and
+// kNT: 16-row blocks a wave.  kW: waves a workgroup.  kShare: the waves have the same rows and
 // divide the keys (and workgroups may too: splits); else each wave has rows of
 // its own and all the keys.  kKT: 16-key tiles a step (even).
-template <int kBits, int kD, int kG, int kNT, bool kShare, int kKT>
+template <int kBits, int kD, int kG, int kNT, bool kShare, int kKT, int kW>
 struct KvAttn {
   static constexpr int kNG = kD / kG;
   static constexpr int kRow = kD * kBits / 8;          // bytes of a token
@@ -295,6 +293,11 @@ struct KvAttn {
     return *reinterpret_cast<const vpart*>(mine + kVAt + t * kTileB + chunk_off(4 * g + i, byte / 16) + byte % 16);
   }
 
+  // lo + mid * step of a value's parameters.
+  static __device__ float middle(uint32_t w) {
+    return fmaf(__uint_as_float(w & 0xFFFF0000u), static_cast<float>(kMidCode<kBits>), bf16_f32(w));
+  }
+
   // ---- one step.  mask: some row does not see some of its keys
   __device__ void compute(int key0, bool mask) {
     // scores, keys x rows
@@ -327,31 +330,44 @@ struct KvAttn {
       }
     }
     if (mask) {
+      bool bad[kKT][4], any = false;
 #pragma unroll
-      for (int t = 0; t < kKT; ++t)
+      for (int t = 0; t < kKT; ++t) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) bad[t][i] = false;
+#pragma unroll
+        for (int gr = 0; gr < kNG; ++gr) {
+          const ev4u vp = params(t, 1, gr);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) bad[t][i] |= !(fabsf(middle(vp[i])) < INFINITY);
+        }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int key = key0 + 16 * t + 4 * g + i;
-          // a value that is not finite must not reach rows that do not see it (0
-          // times it is NaN): those that do get it through their probability
-          bool bad = false;
+          any |= bad[t][i];
 #pragma unroll
-          for (int gr = 0; gr < kNG; ++gr) {
-            const uint32_t w = params(t, 1, gr)[i];
-            const float mid = fmaf(__uint_as_float(w & 0xFFFF0000u), static_cast<float>(kMidCode<kBits>), bf16_f32(w));
-            const bool b = !(fabsf(mid) < INFINITY);
-            if (b) *reinterpret_cast<uint32_t*>(mine + kPAt + 64 * ((t * 2 + 1) * kNG + gr) + 16 * g + 4 * i) = 0;
-            bad |= b;
-          }
-#pragma unroll
-          for (int n = 0; n < kNT; ++n) {
-            if (key < lo[n] || key >= hi[n])
-              S[t][n][i] = -INFINITY;
-            else if (bad)
-              S[t][n][i] = __uint_as_float(0x7FC00000u);
-          }
+          for (int n = 0; n < kNT; ++n)
+            if (key < lo[n] || key >= hi[n]) S[t][n][i] = -INFINITY;
         }
-      wave_fence();
+      }
+      // A value that is not finite must not reach rows that do not see it (0 times
+      // it is NaN): it becomes zero, and those that see it get it through their
+      // probability.
+      if (__any(any)) {
+#pragma unroll
+        for (int t = 0; t < kKT; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (bad[t][i]) {
+#pragma unroll
+              for (int gr = 0; gr < kNG; ++gr)
+                *reinterpret_cast<uint32_t*>(mine + kPAt + 64 * ((t * 2 + 1) * kNG + gr) + 16 * g + 4 * i) = 0;
+#pragma unroll
+              for (int n = 0; n < kNT; ++n)
+                if (S[t][n][i] != -INFINITY) S[t][n][i] = __uint_as_float(0x7FC00000u);
+            }
+        wave_fence();
+      }
     }
     // running maxima
     float top[kNT];
@@ -452,7 +468,7 @@ struct KvAttn {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           vs[i] = __uint_as_float(vp[i] & 0xFFFF0000u);
-          vl[i] = fmaf(vs[i], static_cast<float>(kMidCode<kBits>), bf16_f32(vp[i]));
+          vl[i] = middle(vp[i]);
         }
 #pragma unroll
         for (int n = 0; n < kNT; ++n) {
@@ -541,19 +557,19 @@ struct KvAttn {
     const int tile = a.tiles - 1 - id % a.tiles;  // the longest (last rows of a causal head) first
     id /= a.tiles;
     const int h = id % a.Hkv, b = id / a.Hkv;
+    head = a.cache + static_cast<int64_t>(h) * kv_head_bytes(a.P, kD, kBits, kG);
+    pg = a.pages + b * a.max_pages;
     const int64_t q0 = max(0, min(a.cu_q[b], static_cast<int>(a.T)));
     const int64_t q1 = max(q0, min(static_cast<int64_t>(a.cu_q[b + 1]), a.T));
     const int nq = static_cast<int>(min(q1 - q0, static_cast<int64_t>(a.max_q)));
     const int rows = nq * a.ratio;
-    const int row0 = (kShare ? tile : tile * kAttnWaves + wave) * kRows;
+    const int row0 = (kShare ? tile : tile * kW + wave) * kRows;
     if (row0 >= rows) return;  // uniform over the wave; over the workgroup where waves meet (kShare)
     const int n = static_cast<int>(max(int64_t{0}, min(static_cast<int64_t>(a.kv_lens[b]), a.max_pages * a.P)));
     const int before = n - static_cast<int>(q1 - q0);  // keys before the first query's own
     const int wmax = static_cast<int>(min(a.window, static_cast<int64_t>(1) << 30));
     auto first_key = [&](int row) { return a.window ? max(0, before + row / a.ratio - wmax + 1) : 0; };
     auto end_key = [&](int row) { return a.causal ? max(0, min(n, before + row / a.ratio + 1)) : n; };
-    head = a.cache + static_cast<int64_t>(h) * kv_head_bytes(a.P, kD, kBits, kG);
-    pg = a.pages + b * a.max_pages;
     const int rl = min(row0 + kRows, rows) - 1;  // last row
     // keys that some row sees, and keys that all rows see
     int k0 = first_key(row0) & ~(kKeys - 1), k1 = end_key(rl);
@@ -562,7 +578,7 @@ struct KvAttn {
       k0 += split * a.split_keys;
       k1 = min(k1, k0 + a.split_keys);
     }
-    const int first = k0 + (kShare ? wave * kKeys : 0), hop = kShare ? kAttnWaves * kKeys : kKeys;
+    const int first = k0 + (kShare ? wave * kKeys : 0), hop = kShare ? kW * kKeys : kKeys;
     const int last = k1 - 1;
     // the first step's bytes are on their way while the queries are prepared
     Raw r;
@@ -653,14 +669,14 @@ struct KvAttn {
   // ---- the waves' parts of the same rows, 128 / kNT channels a round.
   // LDS: [wave][row] maxima, sums, factors, then [wave][tile][row][16] outputs
   static constexpr int kTiles = 8 / kNT;  // accumulator tiles a round
-  static constexpr int kJoinB = 3 * kAttnWaves * kRows * 4 + kAttnWaves * kTiles * kRows * 64;
-  static constexpr int kLdsB = kShare && kJoinB > kAttnWaves * kWaveB ? kJoinB : kAttnWaves * kWaveB;
+  static constexpr int kJoinB = 3 * kW * kRows * 4 + kW * kTiles * kRows * 64;
+  static constexpr int kLdsB = kShare && kJoinB > kW * kWaveB ? kJoinB : kW * kWaveB;
   __device__ void join(unsigned char* lds, int split, int rows, int row0, int64_t q0, int h, int wave) {
     constexpr int kRounds = (kD / 16 + kTiles - 1) / kTiles;
     float(*sm)[kRows] = reinterpret_cast<float(*)[kRows]>(lds);
-    float(*sl)[kRows] = sm + kAttnWaves;
-    float* sf = sl[kAttnWaves];  // of each row: 1 / its sum, or 0 (one split: applied here)
-    float(*so)[kTiles][kRows][16] = reinterpret_cast<float(*)[kTiles][kRows][16]>(lds + 3 * kAttnWaves * kRows * 4);
+    float(*sl)[kRows] = sm + kW;
+    float* sf = sl[kW];  // of each row: 1 / its sum, or 0 (one split: applied here)
+    float(*so)[kTiles][kRows][16] = reinterpret_cast<float(*)[kTiles][kRows][16]>(lds + 3 * kW * kRows * 4);
     __syncthreads();  // the waves' own stages end here
     if (g == 0)
 #pragma unroll
@@ -673,10 +689,10 @@ struct KvAttn {
     for (int n = 0; n < kNT; ++n) {
       float mx = -INFINITY, total = 0.0f;
 #pragma unroll
-      for (int w = 0; w < kAttnWaves; ++w) mx = fmaxf(mx, sm[w][16 * n + c16]);
+      for (int w = 0; w < kW; ++w) mx = fmaxf(mx, sm[w][16 * n + c16]);
       const float base = mx == -INFINITY ? 0.0f : mx;
 #pragma unroll
-      for (int w = 0; w < kAttnWaves; ++w)
+      for (int w = 0; w < kW; ++w)
         total += sl[w][16 * n + c16] * __builtin_amdgcn_exp2f(sm[w][16 * n + c16] - base);
       const float f = __builtin_amdgcn_exp2f(m[n] - base);
 #pragma unroll
@@ -708,7 +724,7 @@ struct KvAttn {
       __syncthreads();
       // a thread takes a row's kN neighbouring channels: kN tiles of one group at one of 16
       constexpr int kN = kCh < kTiles ? kCh : kTiles;
-      for (int e = threadIdx.x; e < kTiles / kN * kRows * 16; e += kAttnThreads) {
+      for (int e = threadIdx.x; e < kTiles / kN * kRows * 16; e += 64 * kW) {
         const int i = e % 16, rr = e / 16 % kRows, j = e / 16 / kRows * kN, ti = rd * kTiles + j;
         const int row = row0 + rr;
         if (ti >= kD / 16 || row >= rows) continue;
@@ -717,7 +733,7 @@ struct KvAttn {
         for (int c = 0; c < kN; ++c) {
           v[c] = so[0][j + c][rr][i];
 #pragma unroll
-          for (int w = 1; w < kAttnWaves; ++w) v[c] += so[w][j + c][rr][i];
+          for (int w = 1; w < kW; ++w) v[c] += so[w][j + c][rr][i];
         }
         const int ch = ti / kCh * kG + i * kCh + ti % kCh;
         const int64_t orow = out_row(q0, h, row);
@@ -740,32 +756,35 @@ struct KvAttn {
 
 // Waves a SIMD that the registers have to allow: few rows are bound by memory
 // and want three (168 registers), large heads and many groups would spill at two.
-template <int kD, int kG, int kNT>
-constexpr int kMinWaves = kD == 256 || (kD / kG) * kNT >= 8 ? 1 : kNT == 1 && kD / kG <= 2 ? 3 : 2;
+template <int kD, int kG, int kNT, int kW>
+constexpr int kMinWaves = kW == 8 ? 2 : kD == 256 || (kD / kG) * kNT >= 8 ? 1 : kNT == 1 && kD / kG <= 2 ? 3 : 2;
 
-template <int kBits, int kD, int kG, int kNT, bool kShare, int kKT>
-__global__ __launch_bounds__(kAttnThreads, (kMinWaves<kD, kG, kNT>)) void kv_attn_kernel(KvAttnArgs a) {
-  typedef KvAttn<kBits, kD, kG, kNT, kShare, kKT> K;
+template <int kBits, int kD, int kG, int kNT, bool kShare, int kKT, int kW>
+__global__ __launch_bounds__(64 * kW, (kMinWaves<kD, kG, kNT, kW>)) void kv_attn_kernel(KvAttnArgs a) {
+  typedef KvAttn<kBits, kD, kG, kNT, kShare, kKT, kW> K;
   __shared__ __attribute__((aligned(16))) unsigned char lds[K::kLdsB];
   K k(a);
   k.run(lds);
 }
 
-template <int kBits, int kD, int kG, int kNT, bool kShare>
+template <int kBits, int kD, int kG, int kNT, bool kShare, int kW>
 void launch_nt(const KvAttnArgs& a, hipStream_t st) {
-  constexpr int kKT = kD * kBits <= 512 && kD == kG ? 4 : 2;
+  constexpr int kKT = kD * kBits <= 512 && kD == kG && kW == 4 ? 4 : 2;
   const dim3 grid(static_cast<uint32_t>(static_cast<int64_t>(a.B) * a.Hkv * a.tiles * a.splits));
-  hipLaunchKernelGGL((kv_attn_kernel<kBits, kD, kG, kNT, kShare, kKT>), grid, dim3(kAttnThreads), 0, st, a);
+  hipLaunchKernelGGL((kv_attn_kernel<kBits, kD, kG, kNT, kShare, kKT, kW>), grid, dim3(64 * kW), 0, st, a);
 }
 
 template <int kBits, int kD, int kG>
 fgq_status launch_one(const KvAttnArgs& a, int nt, bool share, hipStream_t st) {
-  if (share && nt == 1)
-    launch_nt<kBits, kD, kG, 1, true>(a, st);
-  else if (share)
-    launch_nt<kBits, kD, kG, 2, true>(a, st);
-  else
-    launch_nt<kBits, kD, kG, 2, false>(a, st);
+  if (!share) {
+    launch_nt<kBits, kD, kG, 2, false, 4>(a, st);
+  } else if (a.wide) {
+    if constexpr (kD < 256 && kD / kG <= 2) nt == 1 ? launch_nt<kBits, kD, kG, 1, true, 8>(a, st) : launch_nt<kBits, kD, kG, 2, true, 8>(a, st);
+  } else if (nt == 1) {
+    launch_nt<kBits, kD, kG, 1, true, 4>(a, st);
+  } else {
+    launch_nt<kBits, kD, kG, 2, true, 4>(a, st);
+  }
   return last_launch();
 }
 

@@ -3,7 +3,7 @@
 //
 // A lane holds eight consecutive channels, so a group of G channels is G / 8
 // neighbouring lanes that agree on its minimum and maximum by exchanges within
-// a row of 16 lanes; one pass over the data, kTokens tokens of a thread in
+// a row of 16 lanes; one pass over the data, several tokens of a thread in
 // flight.  The threads of a workgroup are the eights of a token's heads,
 // several tokens' where those are few, so that the divisions are made once a
 // thread.
@@ -15,13 +15,14 @@
 #include <type_traits>
 
 #include "elem.h"
+#include "igemm.h"
 #include "kvcache.h"
 
 namespace fgq {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kTokens = 4;
+constexpr int kMany = 4;  // tokens a thread, where there are many
 
 struct KvArgs {
   const void* src[2];
@@ -29,32 +30,41 @@ struct KvArgs {
   int64_t st[2], sh[2];  // strides of src in elements: token, head
   const int64_t* slots;
   uint8_t* cache;
-  int64_t T, num_slots;
+  int64_t num_slots;
+  int32_t T;
   int32_t Hkv, D, P, G, row, ng, pshift, gshift;
-  int32_t per;  // tokens a workgroup has at a time (1: a part of one, blockIdx.y)
+  int32_t tokens, heads;  // a workgroup has at a time
   int64_t head_bytes;
+  uint32_t page_bytes;
 };
 
 // Which channels a thread has: head, eighth of the head, and of its
 // workgroup's tokens the first.
 struct Item {
-  int64_t t;
+  int32_t t;
   int h, d8;
   bool have;
 };
+template <int kTok>
 __device__ inline Item item_of(const KvArgs& a) {
-  const uint32_t n8 = a.D / 8, n = a.Hkv * n8;
-  uint32_t col = threadIdx.x, local = 0;
-  if (a.per > 1) {
-    local = col / n;
-    col -= local * n;
-  } else {
-    col += blockIdx.y * kThreads;
-  }
-  const uint32_t h = col / n8;
-  return Item{static_cast<int64_t>(blockIdx.x) * a.per * kTokens + local, static_cast<int>(h),
-              static_cast<int>(col - h * n8), a.per > 1 ? local < static_cast<uint32_t>(a.per) : col < n};
+  const uint32_t n8 = a.D / 8, slot = threadIdx.x / n8, head = slot / a.tokens;
+  const int h = static_cast<int>(blockIdx.y * a.heads + head);
+  return Item{static_cast<int32_t>(blockIdx.x * (a.tokens * kTok) + slot % a.tokens), h,
+              static_cast<int>(threadIdx.x - slot * n8), head < static_cast<uint32_t>(a.heads) && h < a.Hkv};
 }
+
+// Byte offsets of a slot's codes and parameters for this thread; the constant
+// part once, then one 64-bit product a token (the others are of 24 bits).
+struct Place {
+  int64_t codes, params;
+  __device__ Place(const KvArgs& a, const Item& it, int z, int bits) {
+    codes = it.h * a.head_bytes + static_cast<int64_t>(z * a.P) * a.row + it.d8 * bits;
+    params = it.h * a.head_bytes + 2LL * a.P * a.row + 4LL * (z * a.ng + (8 * it.d8 >> a.gshift)) * a.P;
+  }
+  __device__ uint64_t page(const KvArgs& a, int64_t slot) const {
+    return static_cast<uint64_t>(static_cast<uint32_t>(slot >> a.pshift)) * a.page_bytes;
+  }
+};
 
 // The other lanes' value at distance 1, 2 (exchanges within four lanes), 4 and 8
 // (mirrors of 8 and 16, whose quarters agree by then).
@@ -71,24 +81,26 @@ __device__ inline void meet(float& lo, float& hi, float& bad) {
   bad += other<kStep>(bad);
 }
 
-template <int kType, int kBits>
+template <int kType, int kBits, int kTok>
 __global__ __launch_bounds__(kThreads) void kv_write_kernel(KvArgs a) {
 #pragma clang fp contract(off)
   constexpr float L = kBits == 4 ? 15.0f : 255.0f;
   const int z = blockIdx.z;  // 0: keys, 1: values
-  const Item it = item_of(a);
-  const int64_t limit = a.num_slots / a.P * a.Hkv * a.head_bytes;
-  Raw8<kType> raw[kTokens];
-  int64_t slot[kTokens];
+  const Item it = item_of<kTok>(a);
+  const int64_t limit = (a.num_slots >> a.pshift) * a.page_bytes;
+  Raw8<kType> raw[kTok];
+  int64_t slot[kTok];
+  const int64_t src = it.t * a.st[z] + it.h * a.sh[z] + 8 * it.d8, hop = a.tokens * a.st[z];
 #pragma unroll
-  for (int u = 0; u < kTokens; ++u) {
-    const int64_t t = it.t + u * a.per;
+  for (int u = 0; u < kTok; ++u) {
+    const int32_t t = it.t + u * a.tokens;
     const bool have = it.have && t < a.T;
     slot[u] = have ? a.slots[t] : -1;
-    raw[u] = load8<kType>(a.src[z], have ? t * a.st[z] + it.h * a.sh[z] + 8 * it.d8 : 0);
+    raw[u] = load8<kType>(a.src[z], have ? src + u * hop : 0);
   }
+  const Place place(a, it, z, kBits);
 #pragma unroll
-  for (int u = 0; u < kTokens; ++u) {
+  for (int u = 0; u < kTok; ++u) {
     float v[8];
     values8<kType>(raw[u], v);
     float lo = v[0], hi = v[0], bad = 0.0f;
@@ -117,12 +129,10 @@ __global__ __launch_bounds__(kThreads) void kv_write_kernel(KvArgs a) {
     // byte; x >= lo, and the quotient passes L only where the range overflows.
     uint32_t c[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) c[j] = __float_as_uint(fminf((v[j] - lo) * inv, L) + 12582912.0f);
+    for (int j = 0; j < 8; ++j) c[j] = __float_as_uint(__builtin_amdgcn_fmed3f((v[j] - lo) * inv, 0.0f, L) + 12582912.0f);
     if (slot[u] < 0 || slot[u] >= a.num_slots) continue;
-    const int64_t page = slot[u] >> a.pshift;
-    const int at = static_cast<int>(slot[u]) & (a.P - 1);
-    const int64_t base = (page * a.Hkv + it.h) * a.head_bytes;
-    const int64_t cd = base + static_cast<int64_t>(z * a.P + at) * a.row + it.d8 * kBits;
+    const uint32_t at = static_cast<uint32_t>(slot[u]) & (a.P - 1);
+    const int64_t page = place.page(a, slot[u]), cd = page + place.codes + __umul24(at, a.row);
     // bytes of four codes
     auto four = [](uint32_t b0, uint32_t b1, uint32_t b2, uint32_t b3) {
       return __builtin_amdgcn_perm(b1, b0, 0x0C0C0400u) | __builtin_amdgcn_perm(b3, b2, 0x04000C0Cu);
@@ -137,39 +147,38 @@ __global__ __launch_bounds__(kThreads) void kv_write_kernel(KvArgs a) {
       }
     }
     if ((8 * it.d8 & (a.G - 1)) == 0) {
-      const int64_t pp = base + 2LL * a.P * a.row + 4LL * ((z * a.ng + (8 * it.d8 >> a.gshift)) * a.P + at);
+      const int64_t pp = page + place.params + 4 * at;
       if (check_store(kSiteStoreCache, pp, 4, limit)) *reinterpret_cast<uint32_t*>(a.cache + pp) = w >> 16 | t;
     }
   }
 }
 
-template <int kType, int kBits>
+template <int kType, int kBits, int kTok>
 __global__ __launch_bounds__(kThreads) void kv_read_kernel(KvArgs a) {
   const int z = blockIdx.z;
-  const Item it = item_of(a);
+  const Item it = item_of<kTok>(a);
   if (!it.have) return;
-  int64_t slot[kTokens];
+  const Place place(a, it, z, kBits);
+  int64_t slot[kTok];
 #pragma unroll
-  for (int u = 0; u < kTokens; ++u) {
-    const int64_t t = it.t + u * a.per;
+  for (int u = 0; u < kTok; ++u) {
+    const int32_t t = it.t + u * a.tokens;
     slot[u] = t < a.T ? a.slots[t] : -1;
   }
   typedef typename std::conditional<kBits == 4, uint32_t, uint2>::type codes;
-  codes w[kTokens] = {};
-  uint32_t par[kTokens] = {};  // 0: the value 0
+  codes w[kTok] = {};
+  uint32_t par[kTok] = {};  // 0: the value 0
 #pragma unroll
-  for (int u = 0; u < kTokens; ++u)
+  for (int u = 0; u < kTok; ++u)
     if (slot[u] >= 0 && slot[u] < a.num_slots) {
-      const int64_t page = slot[u] >> a.pshift;
-      const int at = static_cast<int>(slot[u]) & (a.P - 1);
-      const uint8_t* base = a.cache + (page * a.Hkv + it.h) * a.head_bytes;
-      w[u] = *reinterpret_cast<const codes*>(base + static_cast<int64_t>(z * a.P + at) * a.row + it.d8 * kBits);
-      par[u] = *reinterpret_cast<const uint32_t*>(
-          base + 2LL * a.P * a.row + 4LL * ((z * a.ng + (8 * it.d8 >> a.gshift)) * a.P + at));
+      const uint32_t at = static_cast<uint32_t>(slot[u]) & (a.P - 1);
+      const uint8_t* page = a.cache + place.page(a, slot[u]);
+      w[u] = *reinterpret_cast<const codes*>(page + place.codes + __umul24(at, a.row));
+      par[u] = *reinterpret_cast<const uint32_t*>(page + place.params + 4 * at);
     }
 #pragma unroll
-  for (int u = 0; u < kTokens; ++u) {
-    const int64_t t = it.t + u * a.per;
+  for (int u = 0; u < kTok; ++u) {
+    const int32_t t = it.t + u * a.tokens;
     if (t >= a.T) break;
     const float lo = bf16_f32(par[u] & 0xFFFFu), step = __uint_as_float(par[u] & 0xFFFF0000u);
     uint32_t even, odd;  // bytes of codes: 4 bits 0 2 4 6 and 1 3 5 7, 8 bits 0 1 2 3 and 4 5 6 7
@@ -186,34 +195,48 @@ __global__ __launch_bounds__(kThreads) void kv_read_kernel(KvArgs a) {
       const uint32_t b = kBits == 4 ? (j % 2 ? odd : even) >> (8 * (j / 2)) : (j < 4 ? even : odd) >> (8 * (j % 4));
       v[j] = fmaf(step, static_cast<float>(b & 0xFFu), lo);
     }
-    const int64_t to = (t * a.Hkv + it.h) * a.D + 8 * it.d8;
-    if (check_store(kSiteStoreY, to, 8, a.T * a.Hkv * a.D)) store8<kType>(a.dst[z], to, v);
+    const int64_t to = (static_cast<int64_t>(t) * a.Hkv + it.h) * a.D + 8 * it.d8;
+    if (check_store(kSiteStoreY, to, 8, static_cast<int64_t>(a.T) * a.Hkv * a.D)) store8<kType>(a.dst[z], to, v);
   }
 }
 
 KvArgs kv_args(const KvGeom& c, int64_t T, const int64_t* slots) {
   KvArgs a{};
   a.slots = slots;
-  a.T = T;
+  a.T = static_cast<int32_t>(T);
   a.num_slots = c.num_pages * c.P;
-  a.pshift = __builtin_ctz(c.P);
-  a.gshift = __builtin_ctz(c.G);
-  const int32_t n = c.Hkv * (c.D / 8);
-  a.per = n <= kThreads / 2 ? kThreads / n : 1;
   a.Hkv = c.Hkv;
   a.D = c.D;
   a.P = c.P;
   a.G = c.G;
+  a.pshift = __builtin_ctz(c.P);
+  a.gshift = __builtin_ctz(c.G);
+  // A wave's lanes are neighbouring tokens of one head where the head has fewer
+  // eights than 64: runs of 256 bytes on either side.
+  const int32_t places = kThreads / (c.D / 8);
+  a.tokens = places < 4 ? 1 : 4;
+  a.heads = places / a.tokens < c.Hkv ? places / a.tokens : c.Hkv;
   a.row = static_cast<int32_t>(kv_row_bytes(c.D, c.bits));
   a.ng = c.D / c.G;
   a.head_bytes = kv_head_bytes(c.P, c.D, c.bits, c.G);
+  a.page_bytes = static_cast<uint32_t>(c.Hkv * a.head_bytes);
   return a;
 }
 
-dim3 kv_grid(const KvArgs& a) {
-  const int32_t n = a.Hkv * (a.D / 8);
-  return dim3(static_cast<uint32_t>(ceil_div(a.T, static_cast<int64_t>(a.per) * kTokens)),
-              a.per > 1 ? 1 : static_cast<uint32_t>(ceil_div(n, kThreads)), 2);
+// fn(integral_constant<tokens a thread>, grid).
+template <typename F>
+void with_grid(const KvArgs& a, F&& fn) {
+  const int64_t parts = 2 * ceil_div(a.Hkv, a.heads);
+  auto grid = [&](int tok) {
+    return dim3(static_cast<uint32_t>(ceil_div(a.T, static_cast<int64_t>(a.tokens) * tok)),
+                static_cast<uint32_t>(parts / 2), 2);
+  };
+  // us, 1 token a thread and 4: 64 tokens written 3.5, 4.3, read 2.6, 3.0; 6007
+  // tokens read 5.6, 4.7; 16384 tokens written 26.5, 24.5, read 18.7, 15.9
+  if (ceil_div(a.T, a.tokens) * parts >= 4LL * ig::device_cus())
+    fn(std::integral_constant<int, kMany>{}, grid(kMany));
+  else
+    fn(std::integral_constant<int, 1>{}, grid(1));
 }
 
 }  // namespace
@@ -228,12 +251,13 @@ fgq_status launch_kv_write(const void* k, const void* v, int32_t type, int64_t T
   a.st[1] = stride[2];
   a.sh[1] = stride[3];
   a.cache = cache;
-  const dim3 grid = kv_grid(a);
   return with_type(type, [&](auto t) {
-    if (c.bits == 4)
-      hipLaunchKernelGGL((kv_write_kernel<decltype(t)::value, 4>), grid, dim3(kThreads), 0, st, a);
-    else
-      hipLaunchKernelGGL((kv_write_kernel<decltype(t)::value, 8>), grid, dim3(kThreads), 0, st, a);
+    with_grid(a, [&](auto tok, dim3 grid) {
+      if (c.bits == 4)
+        hipLaunchKernelGGL((kv_write_kernel<decltype(t)::value, 4, decltype(tok)::value>), grid, dim3(kThreads), 0, st, a);
+      else
+        hipLaunchKernelGGL((kv_write_kernel<decltype(t)::value, 8, decltype(tok)::value>), grid, dim3(kThreads), 0, st, a);
+    });
     return last_launch();
   });
 }
@@ -244,12 +268,13 @@ fgq_status launch_kv_read(const int64_t* slots, int64_t T, const KvGeom& c, cons
   a.dst[0] = k;
   a.dst[1] = v;
   a.cache = const_cast<uint8_t*>(cache);
-  const dim3 grid = kv_grid(a);
   return with_type(type, [&](auto t) {
-    if (c.bits == 4)
-      hipLaunchKernelGGL((kv_read_kernel<decltype(t)::value, 4>), grid, dim3(kThreads), 0, st, a);
-    else
-      hipLaunchKernelGGL((kv_read_kernel<decltype(t)::value, 8>), grid, dim3(kThreads), 0, st, a);
+    with_grid(a, [&](auto tok, dim3 grid) {
+      if (c.bits == 4)
+        hipLaunchKernelGGL((kv_read_kernel<decltype(t)::value, 4, decltype(tok)::value>), grid, dim3(kThreads), 0, st, a);
+      else
+        hipLaunchKernelGGL((kv_read_kernel<decltype(t)::value, 8, decltype(tok)::value>), grid, dim3(kThreads), 0, st, a);
+    });
     return last_launch();
   });
 }
