@@ -114,9 +114,10 @@ struct KvAttn {
   static constexpr int kLB = kRow / 4;                 // bytes of 16 tokens a lane loads
   static constexpr int kLN = kLB >= 16 ? kLB / 16 : 1;
   static constexpr int kPN = (32 * kNG + 63) / 64;     // parameters of 16 tokens a lane loads
-  // a wave's LDS: key codes, value codes, parameters [tile][k, v][group][16]
+  // a wave's LDS: key codes, value codes, parameters as floats [tile][k, v][group]
+  // [step, key: lo, value: lo + mid step][16]
   static constexpr int kTileB = 16 * kRow;
-  static constexpr int kVAt = kKT * kTileB, kPAt = 2 * kKT * kTileB, kWaveB = kPAt + kKT * 128 * kNG;
+  static constexpr int kVAt = kKT * kTileB, kPAt = 2 * kKT * kTileB, kWaveB = kPAt + kKT * 256 * kNG;
   typedef typename std::conditional<kLB == 8, uint2, ev4u>::type piece;
 
   // A step's bytes as they come from memory.
@@ -247,16 +248,25 @@ struct KvAttn {
         *reinterpret_cast<piece*>(mine + kVAt + t * kTileB + off) = r.v[t][j];
       }
     }
+    // one parameter a lane (unpacked by every lane that uses it, it would be by 16)
 #pragma unroll
-    for (int j = 0; j < kPN; ++j)
+    for (int j = 0; j < kPN; ++j) {
+      const int i = 64 * j + lane;  // [k, v][group][16]
+      const float mid = i < 16 * kNG ? 0.0f : static_cast<float>(kMidCode<kBits>);
       if (32 * kNG % 64 == 0 || lane < 32)
 #pragma unroll
-        for (int t = 0; t < kKT; ++t)
-          *reinterpret_cast<uint32_t*>(mine + kPAt + t * 128 * kNG + 4 * (64 * j + lane)) = r.par[t][j];
+        for (int t = 0; t < kKT; ++t) {
+          const float st = __uint_as_float(r.par[t][j] & 0xFFFF0000u);
+          float* p = reinterpret_cast<float*>(mine + kPAt + t * 256 * kNG) + i / 16 * 32 + i % 16;
+          p[0] = st;
+          p[16] = fmaf(st, mid, bf16_f32(r.par[t][j]));
+        }
+    }
   }
 
-  __device__ ev4u params(int t, int z, int gr) const {
-    return *reinterpret_cast<const ev4u*>(mine + kPAt + 64 * ((t * 2 + z) * kNG + gr) + 16 * g);
+  // Four keys' steps (k = 0), and lo or middles (k = 1), of keys (z = 0) or values.
+  __device__ kv4f params(int t, int z, int gr, int k) const {
+    return *reinterpret_cast<const kv4f*>(mine + kPAt + 128 * ((t * 2 + z) * kNG + gr) + 64 * k + 16 * g);
   }
 
   // Words of a key's group (fragment row c16): kKW of them from word g kKW.
@@ -293,11 +303,6 @@ struct KvAttn {
     return *reinterpret_cast<const vpart*>(mine + kVAt + t * kTileB + chunk_off(4 * g + i, byte / 16) + byte % 16);
   }
 
-  // lo + mid * step of a value's parameters.
-  static __device__ float middle(uint32_t w) {
-    return fmaf(__uint_as_float(w & 0xFFFF0000u), static_cast<float>(kMidCode<kBits>), bf16_f32(w));
-  }
-
   // ---- one step.  mask: some row does not see some of its keys
   __device__ void compute(int key0, bool mask) {
     // scores, keys x rows
@@ -308,7 +313,7 @@ struct KvAttn {
       for (int gr = 0; gr < kNG; ++gr) {
         uint32_t kw[kKW];
         key_words(t, gr, kw);
-        const ev4u kp = params(t, 0, gr);
+        const kv4f kst = params(t, 0, gr, 0), kmn = params(t, 0, gr, 1);
         kv4f d[kNT];
 #pragma unroll
         for (int n = 0; n < kNT; ++n) d[n] = kv4f{0, 0, 0, 0};
@@ -321,11 +326,10 @@ struct KvAttn {
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const float st = __uint_as_float(kp[i] & 0xFFFF0000u), mn = bf16_f32(kp[i]);
 #pragma unroll
           for (int n = 0; n < kNT; ++n)
-            S[t][n][i] = gr == 0 ? fmaf(st, d[n][i], mn * qsum[n][gr])
-                                 : fmaf(st, d[n][i], fmaf(mn, qsum[n][gr], S[t][n][i]));
+            S[t][n][i] = gr == 0 ? fmaf(kst[i], d[n][i], kmn[i] * qsum[n][gr])
+                                 : fmaf(kst[i], d[n][i], fmaf(kmn[i], qsum[n][gr], S[t][n][i]));
         }
       }
     }
@@ -337,9 +341,9 @@ struct KvAttn {
         for (int i = 0; i < 4; ++i) bad[t][i] = false;
 #pragma unroll
         for (int gr = 0; gr < kNG; ++gr) {
-          const ev4u vp = params(t, 1, gr);
+          const kv4f mid = params(t, 1, gr, 1);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) bad[t][i] |= !(fabsf(middle(vp[i])) < INFINITY);
+          for (int i = 0; i < 4; ++i) bad[t][i] |= !(fabsf(mid[i]) < INFINITY);
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -360,8 +364,10 @@ struct KvAttn {
           for (int i = 0; i < 4; ++i)
             if (bad[t][i]) {
 #pragma unroll
-              for (int gr = 0; gr < kNG; ++gr)
-                *reinterpret_cast<uint32_t*>(mine + kPAt + 64 * ((t * 2 + 1) * kNG + gr) + 16 * g + 4 * i) = 0;
+              for (int gr = 0; gr < kNG; ++gr) {
+                float* p = reinterpret_cast<float*>(mine + kPAt + 128 * ((t * 2 + 1) * kNG + gr)) + 4 * g + i;
+                p[0] = p[16] = 0.0f;
+              }
 #pragma unroll
               for (int n = 0; n < kNT; ++n)
                 if (S[t][n][i] != -INFINITY) S[t][n][i] = __uint_as_float(0x7FC00000u);
@@ -407,13 +413,9 @@ struct KvAttn {
       for (int n = 0; n < kNT; ++n) y[n] = 0.0f;
 #pragma unroll
       for (int t = 0; t < kKT; ++t) {
-        const ev4u vp = params(t, 1, gr);
-        float s[4];
+        const kv4f s = params(t, 1, gr, 0);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          s[i] = __uint_as_float(vp[i] & 0xFFFF0000u);
-          x = fmaxf(x, s[i]);
-        }
+        for (int i = 0; i < 4; ++i) x = fmaxf(x, s[i]);
         if (mask)  // only of the keys that the row sees
 #pragma unroll
           for (int n = 0; n < kNT; ++n)
@@ -463,13 +465,7 @@ struct KvAttn {
       uint32_t p[kPairs][kNT][4];
 #pragma unroll
       for (int t = 0; t < kKT; ++t) {
-        const ev4u vp = params(t, 1, gr);
-        float vs[4], vl[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          vs[i] = __uint_as_float(vp[i] & 0xFFFF0000u);
-          vl[i] = middle(vp[i]);
-        }
+        const kv4f vs = params(t, 1, gr, 0), vl = params(t, 1, gr, 1);
 #pragma unroll
         for (int n = 0; n < kNT; ++n) {
           float y[4];
@@ -550,10 +546,12 @@ struct KvAttn {
       const int i = min(64 * j + lane, 32 * kNG - 1);  // [k, v][group][16]
       poff[j] = 4 * (i / 16 * a.P + i % 16);
     }
-    // neighbouring workgroups of one sequence and head share its pages in an XCD's L2
-    int id = ig::xcd_swizzle(blockIdx.x, gridDim.x);
-    const int split = id % a.splits;
-    id /= a.splits;
+    // Prompts: neighbouring workgroups, of one sequence and head, read its pages
+    // from one XCD's L2.  Divided keys: nothing is read twice, and a sequence's
+    // heads go to different XCDs, its splits apart, so that long sequences spread.
+    const int per = gridDim.x / a.splits;
+    int id = kShare ? blockIdx.x % per : ig::xcd_swizzle(blockIdx.x, gridDim.x);
+    const int split = kShare ? blockIdx.x / per : 0;
     const int tile = a.tiles - 1 - id % a.tiles;  // the longest (last rows of a causal head) first
     id /= a.tiles;
     const int h = id % a.Hkv, b = id / a.Hkv;
