@@ -20,17 +20,38 @@
 // probabilities have to stand as the second product's operand (the order of
 // the keys inside a sum is free), so nothing moves between lanes but the
 // rows' maxima.  The values' codes go to the same lanes: lane l has channels
-// l % 16 (G / 16) + [0, G / 16) of a group and the same keys, one short load a
-// key; two keys' codes are paired into the halves of a register.
+// l % 16 (G / 16) + [0, G / 16) of a group and the same keys; two keys' codes
+// are paired into the halves of a register.
+//
+// Bytes come as whole runs of a page (16 tokens are one run of codes and 2 D / G
+// short ones of parameters) and reach the lanes that need them through LDS,
+// swizzled; a step's loads are under way while the step before is computed.
+//
+// Few rows (decoding): the four waves of a workgroup have the same rows and
+// take turns at the keys, and workgroups divide long sequences between them.
+// What bounds it is the issue of vector instructions, about 550 for 64 keys of a
+// wave, most of them on the codes (2 MFMA operands' worth for every 8 codes),
+// whatever the number of rows up to 16: 48 sequences of up to 8191 keys, 4 bits,
+// D 128, G 64, are 79 us, 3.7 TB/s of the copy's 5.1.
+//
+// Many rows (prompts): the waves have rows of their own and all need the same
+// fragments, so each makes a quarter of them, in LDS, for all four.  Measured,
+// us, 2 sequences of 2000 queries on 4100 keys, 32 heads on 8, D 128: 316 with
+// every wave on its own, 293 so, 277 with the longest tiles of all heads first
+// (4096 queries on themselves, D 64: 174, 136, 136; D 256: 528, 495, 352).  The
+// rest is the softmax, about 16 vector instructions for 64 scores, next to the
+// products: 37% of the time goes to issuing the former, 19% to the latter, with
+// two waves a SIMD to fill the waits (216 registers).  Four row blocks a wave,
+// one wave a SIMD, took 582 instead of 292.
 //
 // Running maxima are renewed only when a score passes the present one by
 // 2^kSlack (probabilities then reach 2^kSlack, which fp16 has room for), and
 // the values' steps are brought near 1 by a power of two per row and group,
 // renewed when a larger step comes (per row, so that a key that a row does not
-// see leaves it alone whatever its step is); both are rare, so the outputs' accumulators are
-// hardly ever rescaled.  Probabilities times steps are rounded to fp16 (11
-// bits, the range placed so that 2^-25 of the largest is still a normal
-// number); maxima, sums and accumulators are fp32.
+// see leaves it alone whatever its step is); both are rare, so the outputs'
+// accumulators are hardly ever rescaled.  Probabilities times steps are rounded
+// to fp16 (11 bits, the range placed so that 2^-25 of the largest is still a
+// normal number); maxima, sums and accumulators are fp32.
 #pragma once
 
 #include <type_traits>
@@ -46,9 +67,6 @@ typedef float kv4f __attribute__((ext_vector_type(4)));
 
 constexpr float kSlack = 4.0f;     // log2 of how far a score may pass its row's maximum
 constexpr float kBoost = 2048.0f;  // 2^11: the largest rounded probability is 2^(4 + 11)
-#ifndef KT
-#define KT 2
-#endif
 
 __device__ inline kv8h frag(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   return __builtin_bit_cast(kv8h, ev4u{a, b, c, d});
@@ -92,9 +110,9 @@ __device__ inline uint32_t value_pair(uint32_t w, int n) {
   return __builtin_bit_cast(uint32_t, __builtin_bit_cast(v2h, c) + __builtin_bit_cast(v2h, mid));
 }
 
-// kNT: 16-row blocks a wave.  kW: waves a workgroup.  kShare: the waves have the same rows and
-// divide the keys (and workgroups may too: splits); else each wave has rows of
-// its own and all the keys.  kKT: 16-key tiles a step (even).
+// kNT: 16-row blocks a wave.  kW: waves a workgroup.  kShare: the waves have the
+// same rows and divide the keys (and workgroups may too: splits); else each wave
+// has rows of its own and all the keys.  kKT: 16-key tiles a step (even).
 template <int kBits, int kD, int kG, int kNT, bool kShare, int kKT, int kW>
 struct KvAttn {
   static constexpr int kNG = kD / kG;
@@ -118,12 +136,24 @@ struct KvAttn {
   // [step, key: lo, value: lo + mid step][16]
   static constexpr int kTileB = 16 * kRow;
   static constexpr int kVAt = kKT * kTileB, kPAt = 2 * kKT * kTileB, kWaveB = kPAt + kKT * 256 * kNG;
+  // Waves with rows of their own stage together: the codes and the parameters
+  // (of two steps) of the workgroup, and fragments [tile][group][step] of keys,
+  // [tile pair][channel] of values, 1 KB each
+  static constexpr bool kTeam = !kShare;
+  static constexpr int kFAt = kPAt + 2 * kKT * 256 * kNG, kFVAt = kFAt + kKT * kNG * kSteps * 1024;
+  static constexpr int kTeamB = kFVAt + kPairs * (kD / 16) * 1024;
   typedef typename std::conditional<kLB == 8, uint2, ev4u>::type piece;
 
   // A step's bytes as they come from memory.
   struct Raw {
     piece k[kKT][kLN], v[kKT][kLN];
     uint32_t par[kKT][kPN];
+  };
+
+  // A wave's share of it where they stage together: one tile.
+  struct TeamRaw {
+    piece k[kLN], v[kLN];
+    uint32_t par[kPN];
   };
 
   // LDS offset of a chunk of one of 16 tokens.  Swizzled: the fragment reads of
@@ -138,7 +168,8 @@ struct KvAttn {
 
   const KvAttnArgs& a;
   int lane, c16, g;
-  unsigned char* mine;         // the wave's LDS
+  unsigned char* mine;         // the wave's LDS (or the workgroup's: kTeam)
+  int odd;                     // where the step's parameters are there (kTeam)
   uint32_t poff[kPN];          // where this lane's parameters of 16 tokens lie
   const uint8_t* head;         // cache + this key head
   const int32_t* pg;           // the sequence's pages
@@ -198,34 +229,38 @@ struct KvAttn {
   // ---- one step's bytes: 16 tokens at a time, whole runs of a page.  last: the
   // largest key whose page is known to be the sequence's own
   __device__ void load(Raw& r, int key0, int last) const {
-    // the bytes of this head in the page that holds `key`
-    auto page_of = [&](int key) {
-      const int pid = __builtin_amdgcn_readfirstlane(pg[key >> a.pshift]);
-      // a page number outside the cache reads page 0 instead of foreign memory
-      const int64_t page = static_cast<uint32_t>(pid) < static_cast<uint32_t>(a.num_pages) ? pid : 0;
-      return make_buf(head + page * a.page_bytes, 2 * a.P * (kRow + 4 * kNG), kSiteCache, ig::kBufFlags);
-    };
-    auto tile = [&](const Buf& pgb, int t, int at) {
-#pragma unroll
-      for (int j = 0; j < kLN; ++j) {
-        r.k[t][j] = get(pgb, 1024 * j + static_cast<int>(sizeof(piece)) * lane, at * kRow);
-        r.v[t][j] = get(pgb, 1024 * j + static_cast<int>(sizeof(piece)) * lane, (a.P + at) * kRow);
-      }
-#pragma unroll
-      for (int j = 0; j < kPN; ++j) r.par[t][j] = buf_load_b32(pgb, poff[j], 2 * a.P * kRow + 4 * at);
-    };
     if (a.P >= kKeys) {  // steps are aligned to kKeys: one page
-      const int key = min(key0, last);
-      const Buf pgb = page_of(key);
+      const Buf pgb = page_of(min(key0, last));
 #pragma unroll
-      for (int t = 0; t < kKT; ++t) tile(pgb, t, (key0 & (a.P - 1)) + 16 * t);
+      for (int t = 0; t < kKT; ++t) load_tile(pgb, (key0 & (a.P - 1)) + 16 * t, r.k[t], r.v[t], r.par[t]);
     } else {
 #pragma unroll
       for (int t = 0; t < kKT; ++t) {
         const int key = min(key0 + 16 * t, last & ~15);
-        tile(page_of(key), t, key & (a.P - 1));
+        load_tile(page_of(key), key & (a.P - 1), r.k[t], r.v[t], r.par[t]);
       }
     }
+  }
+  __device__ void load(TeamRaw& r, int key0, int last, int wave) const {
+    if (wave >= kKT) return;
+    const int key = min(key0 + 16 * wave, last & ~15);
+    load_tile(page_of(key), key & (a.P - 1), r.k, r.v, r.par);
+  }
+  // The bytes of this head in the page that holds `key`.
+  __device__ Buf page_of(int key) const {
+    const int pid = __builtin_amdgcn_readfirstlane(pg[key >> a.pshift]);
+    // a page number outside the cache reads page 0 instead of foreign memory
+    const int64_t page = static_cast<uint32_t>(pid) < static_cast<uint32_t>(a.num_pages) ? pid : 0;
+    return make_buf(head + page * a.page_bytes, 2 * a.P * (kRow + 4 * kNG), kSiteCache, ig::kBufFlags);
+  }
+  __device__ void load_tile(const Buf& pgb, int at, piece (&k)[kLN], piece (&v)[kLN], uint32_t (&p)[kPN]) const {
+#pragma unroll
+    for (int j = 0; j < kLN; ++j) {
+      k[j] = get(pgb, 1024 * j + static_cast<int>(sizeof(piece)) * lane, at * kRow);
+      v[j] = get(pgb, 1024 * j + static_cast<int>(sizeof(piece)) * lane, (a.P + at) * kRow);
+    }
+#pragma unroll
+    for (int j = 0; j < kPN; ++j) p[j] = buf_load_b32(pgb, poff[j], 2 * a.P * kRow + 4 * at);
   }
   static __device__ piece get(const Buf& b, uint32_t voff, uint32_t soff) {
     if constexpr (kLB == 8) {
@@ -236,37 +271,106 @@ struct KvAttn {
     }
   }
 
-  // ---- into the wave's LDS
-  __device__ void stage(const Raw& r) const {
-#pragma unroll
-    for (int j = 0; j < kLN; ++j) {
-      const int byte = 1024 * j + static_cast<int>(sizeof(piece)) * lane;
-      const int off = chunk_off(byte / kRow, byte % kRow / 16) + byte % 16;
-#pragma unroll
-      for (int t = 0; t < kKT; ++t) {
-        *reinterpret_cast<piece*>(mine + t * kTileB + off) = r.k[t][j];
-        *reinterpret_cast<piece*>(mine + kVAt + t * kTileB + off) = r.v[t][j];
-      }
-    }
-    // one parameter a lane (unpacked by every lane that uses it, it would be by 16)
+  // ---- into LDS
+  __device__ unsigned char* params_at() const { return mine + kPAt + (kTeam ? odd : 0); }
+  __device__ void put_codes(int t, int j, piece k, piece v) const {
+    const int byte = 1024 * j + static_cast<int>(sizeof(piece)) * lane;
+    const int off = chunk_off(byte / kRow, byte % kRow / 16) + byte % 16;
+    *reinterpret_cast<piece*>(mine + t * kTileB + off) = k;
+    *reinterpret_cast<piece*>(mine + kVAt + t * kTileB + off) = v;
+  }
+  // One parameter a lane (unpacked by every lane that uses it, it would be by 16).
+  __device__ void put_params(int t, const uint32_t (&raw)[kPN]) const {
 #pragma unroll
     for (int j = 0; j < kPN; ++j) {
       const int i = 64 * j + lane;  // [k, v][group][16]
-      const float mid = i < 16 * kNG ? 0.0f : static_cast<float>(kMidCode<kBits>);
-      if (32 * kNG % 64 == 0 || lane < 32)
-#pragma unroll
-        for (int t = 0; t < kKT; ++t) {
-          const float st = __uint_as_float(r.par[t][j] & 0xFFFF0000u);
-          float* p = reinterpret_cast<float*>(mine + kPAt + t * 256 * kNG) + i / 16 * 32 + i % 16;
-          p[0] = st;
-          p[16] = fmaf(st, mid, bf16_f32(r.par[t][j]));
-        }
+      const float st = __uint_as_float(raw[j] & 0xFFFF0000u);
+      const float other = fmaf(st, i >= 16 * kNG ? static_cast<float>(kMidCode<kBits>) : 0.0f, bf16_f32(raw[j]));
+      if (32 * kNG % 64 == 0 || lane < 32) {
+        float* p = reinterpret_cast<float*>(params_at() + t * 256 * kNG) + i / 16 * 32 + i % 16;
+        p[0] = st;
+        p[16] = other;
+      }
     }
+  }
+  // A value that is not finite must not reach rows that do not see it (0 times it
+  // is NaN): its parameters become zero and its key's step NaN, so that the rows
+  // that see it get it through their score.
+  __device__ void hide_values() const {
+#pragma unroll
+    for (int t = 0; t < kKT; ++t) hide_values(t);
+    wave_fence();
+  }
+  __device__ void hide_values(int t) const {
+    float* const base = reinterpret_cast<float*>(params_at() + t * 256 * kNG);
+    for (int i = lane; i < 16 * kNG; i += 64) {
+      float* p = base + (kNG + i / 16) * 32 + i % 16;
+      if (!(fabsf(p[16]) < INFINITY)) {
+        p[0] = p[16] = 0.0f;
+        base[i % 16] = __uint_as_float(0x7FC00000u);
+      }
+    }
+  }
+  __device__ void stage(const Raw& r) const {
+#pragma unroll
+    for (int j = 0; j < kLN; ++j) {
+#pragma unroll
+      for (int t = 0; t < kKT; ++t) put_codes(t, j, r.k[t][j], r.v[t][j]);
+    }
+#pragma unroll
+    for (int t = 0; t < kKT; ++t) put_params(t, r.par[t]);
+  }
+  __device__ void stage(const TeamRaw& r, int wave) const {
+    if (wave >= kKT) return;
+#pragma unroll
+    for (int j = 0; j < kLN; ++j) put_codes(wave, j, r.k[j], r.v[j]);
+    put_params(wave, r.par);
+  }
+
+  // ---- the waves together: fragments from the staged codes, a part each
+  __device__ unsigned char* key_frag_at(int t, int gr, int s) const {
+    return mine + kFAt + ((t * kNG + gr) * kSteps + s) * 1024 + 16 * lane;
+  }
+  __device__ unsigned char* value_frag_at(int u, int ch) const {
+    return mine + kFVAt + (u * (kD / 16) + ch) * 1024 + 16 * lane;
+  }
+  __device__ void expand(int wave) const {
+    for (int it = wave; it < kKT * kNG; it += kW) {
+      const int t = it / kNG, gr = it % kNG;
+      uint32_t kw[kKW];
+      key_words(t, gr, kw);
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s) *reinterpret_cast<kv8h*>(key_frag_at(t, gr, s)) = key_step(kw, s);
+    }
+    typedef typename std::conditional<kVB == 1, uint8_t, uint16_t>::type half;
+    for (int it = wave; it < kPairs * kNG * kVP; it += kW) {  // 16 bits of each key of a pair of tiles
+      const int pc = it % kVP, gr = it / kVP % kNG, u = it / (kVP * kNG);
+      const int byte = gr * kGB + c16 * kVB + 2 * pc;
+      uint32_t w[4];
+#pragma unroll
+      for (int h = 0; h < 4; ++h) {
+        uint32_t x[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+          x[e] = *reinterpret_cast<const half*>(mine + kVAt + (2 * u + h / 2) * kTileB +
+                                                chunk_off(4 * g + 2 * (h % 2) + e, byte / 16) + byte % 16);
+        w[h] = x[0] | x[1] << 16;
+      }
+      constexpr int kN = kCh < kPer ? kCh : kPer;
+#pragma unroll
+      for (int e = 0; e < kN; ++e)
+        *reinterpret_cast<kv8h*>(value_frag_at(u, gr * kCh + pc * kPer + e)) =
+            frag(value_pair<kBits>(w[0], e), value_pair<kBits>(w[1], e), value_pair<kBits>(w[2], e),
+                 value_pair<kBits>(w[3], e));
+    }
+  }
+  static __device__ kv8h key_step(const uint32_t (&kw)[kKW], int s) {
+    return kBits == 4 ? key_frag<kBits>(kw[s % kKW], 0) : key_frag<kBits>(kw[(2 * s) % kKW], kw[(2 * s + 1) % kKW]);
   }
 
   // Four keys' steps (k = 0), and lo or middles (k = 1), of keys (z = 0) or values.
   __device__ kv4f params(int t, int z, int gr, int k) const {
-    return *reinterpret_cast<const kv4f*>(mine + kPAt + 128 * ((t * 2 + z) * kNG + gr) + 64 * k + 16 * g);
+    return *reinterpret_cast<const kv4f*>(params_at() + 128 * ((t * 2 + z) * kNG + gr) + 64 * k + 16 * g);
   }
 
   // Words of a key's group (fragment row c16): kKW of them from word g kKW.
@@ -312,15 +416,18 @@ struct KvAttn {
 #pragma unroll
       for (int gr = 0; gr < kNG; ++gr) {
         uint32_t kw[kKW];
-        key_words(t, gr, kw);
+        if constexpr (!kTeam) key_words(t, gr, kw);
         const kv4f kst = params(t, 0, gr, 0), kmn = params(t, 0, gr, 1);
         kv4f d[kNT];
 #pragma unroll
         for (int n = 0; n < kNT; ++n) d[n] = kv4f{0, 0, 0, 0};
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) {
-          const kv8h kf = kBits == 4 ? key_frag<kBits>(kw[s % kKW], 0)
-                                     : key_frag<kBits>(kw[(2 * s) % kKW], kw[(2 * s + 1) % kKW]);
+          kv8h kf;
+          if constexpr (kTeam)
+            kf = *reinterpret_cast<const kv8h*>(key_frag_at(t, gr, s));
+          else
+            kf = key_step(kw, s);
 #pragma unroll
           for (int n = 0; n < kNT; ++n) d[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, q[n][gr][s], d[n], 0, 0, 0);
         }
@@ -333,48 +440,16 @@ struct KvAttn {
         }
       }
     }
-    if (mask) {
-      bool bad[kKT][4], any = false;
+    if (mask)
 #pragma unroll
-      for (int t = 0; t < kKT; ++t) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) bad[t][i] = false;
-#pragma unroll
-        for (int gr = 0; gr < kNG; ++gr) {
-          const kv4f mid = params(t, 1, gr, 1);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) bad[t][i] |= !(fabsf(mid[i]) < INFINITY);
-        }
+      for (int t = 0; t < kKT; ++t)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int key = key0 + 16 * t + 4 * g + i;
-          any |= bad[t][i];
 #pragma unroll
           for (int n = 0; n < kNT; ++n)
             if (key < lo[n] || key >= hi[n]) S[t][n][i] = -INFINITY;
         }
-      }
-      // A value that is not finite must not reach rows that do not see it (0 times
-      // it is NaN): it becomes zero, and those that see it get it through their
-      // probability.
-      if (__any(any)) {
-#pragma unroll
-        for (int t = 0; t < kKT; ++t)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (bad[t][i]) {
-#pragma unroll
-              for (int gr = 0; gr < kNG; ++gr) {
-                float* p = reinterpret_cast<float*>(mine + kPAt + 128 * ((t * 2 + 1) * kNG + gr)) + 4 * g + i;
-                p[0] = p[16] = 0.0f;
-              }
-#pragma unroll
-              for (int n = 0; n < kNT; ++n)
-                if (S[t][n][i] != -INFINITY) S[t][n][i] = __uint_as_float(0x7FC00000u);
-            }
-        wave_fence();
-      }
-    }
     // running maxima
     float top[kNT];
     bool renew = false;
@@ -485,8 +560,9 @@ struct KvAttn {
         for (int n = 0; n < kNT; ++n) pf[n] = frag(p[u][n][0], p[u][n][1], p[u][n][2], p[u][n][3]);
         uint32_t w[4][kVP];  // key pairs (0,1) (2,3) of both tiles
 #pragma unroll
-        for (int h = 0; h < 4; ++h) {
-          const vpart x = value_part(2 * u + h / 2, 2 * (h % 2), gr), y = value_part(2 * u + h / 2, 2 * (h % 2) + 1, gr);
+        for (int h = 0; h < (kTeam ? 0 : 4); ++h) {
+          const int t = 2 * u + h / 2, i = 2 * (h % 2);
+          const vpart x = value_part(t, i, gr), y = value_part(t, i + 1, gr);
           if constexpr (kVB <= 2) {
             w[h][0] = static_cast<uint32_t>(x) | static_cast<uint32_t>(y) << 16;
           } else if constexpr (kVB == 4) {
@@ -502,8 +578,12 @@ struct KvAttn {
 #pragma unroll
         for (int c = 0; c < kCh; ++c) {
           const int pc = c / kPer, e = c % kPer;
-          const kv8h vf = frag(value_pair<kBits>(w[0][pc], e), value_pair<kBits>(w[1][pc], e),
-                               value_pair<kBits>(w[2][pc], e), value_pair<kBits>(w[3][pc], e));
+          kv8h vf;
+          if constexpr (kTeam)
+            vf = *reinterpret_cast<const kv8h*>(value_frag_at(u, gr * kCh + c));
+          else
+            vf = frag(value_pair<kBits>(w[0][pc], e), value_pair<kBits>(w[1][pc], e), value_pair<kBits>(w[2][pc], e),
+                      value_pair<kBits>(w[3][pc], e));
 #pragma unroll
           for (int n = 0; n < kNT; ++n)
             acc[n][gr * kCh + c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pf[n], acc[n][gr * kCh + c], 0, 0, 0);
@@ -540,29 +620,32 @@ struct KvAttn {
     c16 = lane % 16;
     g = lane / 16;
     const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
-    mine = lds + wave * kWaveB;
+    mine = kTeam ? lds : lds + wave * kWaveB;
+    odd = 0;
 #pragma unroll
     for (int j = 0; j < kPN; ++j) {
       const int i = min(64 * j + lane, 32 * kNG - 1);  // [k, v][group][16]
       poff[j] = 4 * (i / 16 * a.P + i % 16);
     }
-    // Prompts: neighbouring workgroups, of one sequence and head, read its pages
-    // from one XCD's L2.  Divided keys: nothing is read twice, and a sequence's
-    // heads go to different XCDs, its splits apart, so that long sequences spread.
-    const int per = gridDim.x / a.splits;
-    int id = kShare ? blockIdx.x % per : ig::xcd_swizzle(blockIdx.x, gridDim.x);
-    const int split = kShare ? blockIdx.x / per : 0;
-    const int tile = a.tiles - 1 - id % a.tiles;  // the longest (last rows of a causal head) first
-    id /= a.tiles;
-    const int h = id % a.Hkv, b = id / a.Hkv;
+    // Divided keys: nothing is read twice, and a sequence's heads go to different
+    // XCDs, its splits apart, so that long sequences spread.  Prompts: the longest
+    // tiles (last rows of a causal head) of every head first; 8, 16, ... heads of
+    // all sequences keep a head's tiles, which read the same pages, on one XCD.
+    const int per = gridDim.x / a.splits, heads = per / a.tiles;
+    const int id = blockIdx.x % per, split = blockIdx.x / per;
+    const int tile = a.tiles - 1 - (kShare ? id % a.tiles : id / heads);
+    const int hb = kShare ? id / a.tiles : id % heads;
+    const int h = hb % a.Hkv, b = hb / a.Hkv;
     head = a.cache + static_cast<int64_t>(h) * kv_head_bytes(a.P, kD, kBits, kG);
     pg = a.pages + b * a.max_pages;
     const int64_t q0 = max(0, min(a.cu_q[b], static_cast<int>(a.T)));
     const int64_t q1 = max(q0, min(static_cast<int64_t>(a.cu_q[b + 1]), a.T));
     const int nq = static_cast<int>(min(q1 - q0, static_cast<int64_t>(a.max_q)));
     const int rows = nq * a.ratio;
-    const int row0 = (kShare ? tile : tile * kW + wave) * kRows;
-    if (row0 >= rows) return;  // uniform over the wave; over the workgroup where waves meet (kShare)
+    const int wg0 = tile * (kShare ? 1 : kW) * kRows;  // the workgroup's first row
+    if (wg0 >= rows) return;
+    const int row0 = kShare ? wg0 : min(wg0 + wave * kRows, rows - 1);  // (kTeam: waves past the rows repeat the last)
+    const bool idle = kTeam && wg0 + wave * kRows >= rows;
     const int n = static_cast<int>(max(int64_t{0}, min(static_cast<int64_t>(a.kv_lens[b]), a.max_pages * a.P)));
     const int before = n - static_cast<int>(q1 - q0);  // keys before the first query's own
     const int wmax = static_cast<int>(min(a.window, static_cast<int64_t>(1) << 30));
@@ -570,17 +653,24 @@ struct KvAttn {
     auto end_key = [&](int row) { return a.causal ? max(0, min(n, before + row / a.ratio + 1)) : n; };
     const int rl = min(row0 + kRows, rows) - 1;  // last row
     // keys that some row sees, and keys that all rows see
-    int k0 = first_key(row0) & ~(kKeys - 1), k1 = end_key(rl);
+    int k0 = first_key(row0) & ~(kKeys - 1), k1 = idle ? 0 : end_key(rl);
     const int all0 = first_key(rl), all1 = end_key(row0);
     if (a.splits > 1) {
       k0 += split * a.split_keys;
       k1 = min(k1, k0 + a.split_keys);
     }
-    const int first = k0 + (kShare ? wave * kKeys : 0), hop = kShare ? kW * kKeys : kKeys;
-    const int last = k1 - 1;
+    // this wave's steps; where the waves stage together, those of all their rows
+    const int first = kTeam ? first_key(wg0) & ~(kKeys - 1) : k0 + wave * kKeys, hop = kTeam ? kKeys : kW * kKeys;
+    const int wgl = min(wg0 + kW * kRows, rows) - 1;
+    const int end = kTeam ? end_key(wgl) : k1, last = end - 1;
     // the first step's bytes are on their way while the queries are prepared
-    Raw r;
-    if (first < k1) load(r, first, last);
+    typename std::conditional<kTeam, TeamRaw, Raw>::type r;
+    if (first < end) {
+      if constexpr (kTeam)
+        load(r, first, last, wave);
+      else
+        load(r, first, last);
+    }
 #pragma unroll
     for (int t = 0; t < kNT; ++t) {
       const int row = min(row0 + 16 * t + c16, rl);
@@ -598,17 +688,34 @@ struct KvAttn {
 #pragma unroll
       for (int j = 0; j < kD / 16; ++j) acc[t][j] = kv4f{0, 0, 0, 0};
     }
-    for (int key = first; key < k1; key += hop) {
-      stage(r);
-      if (key + hop < k1) load(r, key + hop, last);
-      wave_fence();
-      compute(key, key < all0 || key + kKeys > min(all1, k1));
-      wave_fence();
+    for (int key = first; key < end; key += hop) {
+      if constexpr (kTeam) {
+        stage(r, wave);
+        if ((key < first_key(wgl) || key + kKeys > end_key(wg0)) && wave < kKT) {
+          wave_fence();
+          hide_values(wave);
+        }
+        __syncthreads();  // the codes are there, and the last step's fragments done with
+        if (key + hop < end) load(r, key + hop, last, wave);
+        expand(wave);
+        __syncthreads();
+        if (key + kKeys > k0 && key < k1) compute(key, key < all0 || key + kKeys > min(all1, k1));
+        // the others may still read this step's parameters when the next one's come
+        odd ^= kKT * 256 * kNG;
+      } else {
+        const bool mask = key < all0 || key + kKeys > min(all1, k1);
+        stage(r);
+        if (key + hop < end) load(r, key + hop, last);
+        wave_fence();
+        if (mask) hide_values();
+        compute(key, mask);
+        wave_fence();
+      }
     }
     finish();
     if constexpr (kShare)
       join(lds, split, rows, row0, q0, h, wave);
-    else
+    else if (!idle)
       store(rows, row0, q0, h);
   }
 
@@ -668,7 +775,7 @@ struct KvAttn {
   // LDS: [wave][row] maxima, sums, factors, then [wave][tile][row][16] outputs
   static constexpr int kTiles = 8 / kNT;  // accumulator tiles a round
   static constexpr int kJoinB = 3 * kW * kRows * 4 + kW * kTiles * kRows * 64;
-  static constexpr int kLdsB = kShare && kJoinB > kW * kWaveB ? kJoinB : kW * kWaveB;
+  static constexpr int kLdsB = kTeam ? kTeamB : kJoinB > kW * kWaveB ? kJoinB : kW * kWaveB;
   __device__ void join(unsigned char* lds, int split, int rows, int row0, int64_t q0, int h, int wave) {
     constexpr int kRounds = (kD / 16 + kTiles - 1) / kTiles;
     float(*sm)[kRows] = reinterpret_cast<float(*)[kRows]>(lds);
@@ -767,7 +874,7 @@ __global__ __launch_bounds__(64 * kW, (kMinWaves<kD, kG, kNT, kW>)) void kv_attn
 
 template <int kBits, int kD, int kG, int kNT, bool kShare, int kW>
 void launch_nt(const KvAttnArgs& a, hipStream_t st) {
-  constexpr int kKT = kD * kBits <= 512 && kD == kG && kW == 4 ? 4 : 2;
+  constexpr int kKT = !kShare ? 4 : kD * kBits <= 512 && kD == kG && kW == 4 ? 4 : 2;
   const dim3 grid(static_cast<uint32_t>(static_cast<int64_t>(a.B) * a.Hkv * a.tiles * a.splits));
   hipLaunchKernelGGL((kv_attn_kernel<kBits, kD, kG, kNT, kShare, kKT, kW>), grid, dim3(64 * kW), 0, st, a);
 }
@@ -777,7 +884,12 @@ fgq_status launch_one(const KvAttnArgs& a, int nt, bool share, hipStream_t st) {
   if (!share) {
     launch_nt<kBits, kD, kG, 2, false, 4>(a, st);
   } else if (a.wide) {
-    if constexpr (kD < 256 && kD / kG <= 2) nt == 1 ? launch_nt<kBits, kD, kG, 1, true, 8>(a, st) : launch_nt<kBits, kD, kG, 2, true, 8>(a, st);
+    if constexpr (kD < 256 && kD / kG <= 2) {
+      if (nt == 1)
+        launch_nt<kBits, kD, kG, 1, true, 8>(a, st);
+      else
+        launch_nt<kBits, kD, kG, 2, true, 8>(a, st);
+    }
   } else if (nt == 1) {
     launch_nt<kBits, kD, kG, 1, true, 4>(a, st);
   } else {
