@@ -32,7 +32,7 @@ def run_cases(fgq, torch):
     # cache and attention
     layouts = [(64, 4, 32), (64, 8, 64), (128, 4, 128), (128, 4, 64), (128, 8, 32), (256, 4, 64), (256, 8, 128)]
     seqs = [[(700, 1), (0, 1), (33, 1)], [(100, 40), (20, 33)], [(300, 3), (5, 5)], [(3000, 1), (40, 1)],
-            [(500, 140), (1, 1)]]
+            [(500, 140), (1, 1)], [(200, 90), (33, 70)] + [(b % 5, b % 2) for b in range(260)]]
     for i, (D, bits, G) in enumerate(layouts):
         for j, sq in enumerate(seqs):
             Hkv, ratio, P = 1 + (i + j) % 3, (1, 4, 3)[j % 3], (16, 32, 64, 128)[(i + j) % 4]
