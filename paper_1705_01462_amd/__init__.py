@@ -577,7 +577,7 @@ def _type(t, name):
 
 
 # As above, a call's arguments are looked at in one pass where they are as they
-# should be (a call's Python costs as much as its launch: 10.7 -> 7.3 us for a
+# should be (a call's Python costs as much as its launch: 10.7 -> 8.3 us for a
 # product of one row).
 
 def _gpu(t, dtype, name):

@@ -105,10 +105,10 @@ struct Plan {
 // 553; 2048 on 8192 (512) 426, 511.  Heads of 256, on 8192: 512 queries 882, 585;
 // 768 882, 858; 1024 on 16384 1753, 2211.
 //
-// Three workgroups fit a unit, so keys are split until there are that many (us,
-// two sequences of 131072 keys and 16 (sequence, key head) pairs: 1.5 a unit 89,
-// 3 72, 6 80, 12 89; 48 sequences of up to 8191: 90, 82, 91, 99), but not below
-// 256 keys, a step of each of four waves.
+// Keys are split until there are three workgroups a unit (us, two sequences of
+// 131072 keys and 16 (sequence, key head) pairs: 1.5 a unit 88, 3 70, 6 80, 12
+// 88; 48 sequences of up to 8191: 85, 80, 82, 84), but not below 256 keys, two
+// steps of each of four waves.
 Plan plan(int32_t D, bool wide, int32_t Hq, int32_t Hkv, int64_t B, int64_t max_q, int64_t max_keys, int64_t window) {
   Plan p{};
   const int64_t rows = max_q * (Hq / Hkv), cus = ig::device_cus();
@@ -122,8 +122,8 @@ Plan plan(int32_t D, bool wide, int32_t Hq, int32_t Hkv, int64_t B, int64_t max_
     const int64_t wgs = B * Hkv * p.tiles;
     p.splits = static_cast<int>(std::max<int64_t>(1, std::min({keys / kKvAttnSplit, 3 * cus / wgs, int64_t{1024}})));
     // Some hundred keys and few workgroups: eight waves take them without a join
-    // (us: 8 pairs of 777 keys 12.5 instead of 13.9, 192 pairs of a window of 512
-    // 12.3 instead of 17.4; 64 pairs of 4096 keys 36 instead of 22.5).
+    // (us: 8 pairs of 777 keys 11.7 instead of 13.7, 192 pairs of a window of 512
+    // 11.5 instead of 15.9; 64 pairs of 4096 keys 34 instead of 19.4).
     if (wide && wgs <= cus && keys > 256 && keys <= 1024) {
       p.wide = true;
       p.splits = 1;

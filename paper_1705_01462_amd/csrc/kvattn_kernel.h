@@ -32,7 +32,7 @@
 // What bounds it is the issue of vector instructions, about 550 for 64 keys of a
 // wave, most of them on the codes (2 MFMA operands' worth for every 8 codes),
 // whatever the number of rows up to 16: 48 sequences of up to 8191 keys, 4 bits,
-// D 128, G 64, are 79 us, 3.7 TB/s of the copy's 5.1.
+// D 128, G 128, are 77 us, 3.8 TB/s of the copy's 5.1.
 //
 // Many rows (prompts): the waves have rows of their own and all need the same
 // fragments, so each makes a quarter of them, in LDS, for all four.  Measured,
@@ -112,8 +112,8 @@ __device__ inline uint32_t value_pair(uint32_t w, int n) {
 
 // kNT: 16-row blocks a wave.  kW: waves a workgroup.  kShare: the waves have the
 // same rows and divide the keys (and workgroups may too: splits); else each wave
-// has rows of its own and all the keys.  kKT: 16-key tiles a step (even).
-template <int kBits, int kD, int kG, int kNT, bool kShare, int kKT, int kW>
+// has rows of its own and all the keys.
+template <int kBits, int kD, int kG, int kNT, bool kShare, int kW>
 struct KvAttn {
   static constexpr int kNG = kD / kG;
   static constexpr int kRow = kD * kBits / 8;          // bytes of a token
@@ -125,6 +125,10 @@ struct KvAttn {
   static constexpr int kCh = kG / 16;                  // channels of a group a lane has
   static constexpr int kPer = kBits == 4 ? 4 : 2;      // channels a piece
   static constexpr int kRows = 16 * kNT;
+  // 16-key tiles a step (even).  Four where the keys are divided (us): 48
+  // sequences of up to 8191 keys, D 128, 4 bits 80 instead of 77, D 64, 8 bits 74
+  // instead of 68, 4 bits 52 instead of 54.
+  static constexpr int kKT = kShare ? 2 : 4;
   static constexpr int kKeys = 16 * kKT;
   static constexpr int kPairs = kKT / 2;
 
@@ -859,14 +863,14 @@ struct KvAttn {
   }
 };
 
-// Waves a SIMD that the registers have to allow: few rows are bound by memory
-// and want three (168 registers), large heads and many groups would spill at two.
+// Waves a SIMD that the registers have to allow: large heads and many groups
+// would spill at two (three for few rows: no faster).
 template <int kD, int kG, int kNT, int kW>
-constexpr int kMinWaves = kW == 8 ? 2 : kD == 256 || (kD / kG) * kNT >= 8 ? 1 : kNT == 1 && kD / kG <= 2 ? 3 : 2;
+constexpr int kMinWaves = kW == 4 && (kD == 256 || (kD / kG) * kNT >= 8) ? 1 : 2;
 
-template <int kBits, int kD, int kG, int kNT, bool kShare, int kKT, int kW>
+template <int kBits, int kD, int kG, int kNT, bool kShare, int kW>
 __global__ __launch_bounds__(64 * kW, (kMinWaves<kD, kG, kNT, kW>)) void kv_attn_kernel(KvAttnArgs a) {
-  typedef KvAttn<kBits, kD, kG, kNT, kShare, kKT, kW> K;
+  typedef KvAttn<kBits, kD, kG, kNT, kShare, kW> K;
   __shared__ __attribute__((aligned(16))) unsigned char lds[K::kLdsB];
   K k(a);
   k.run(lds);
@@ -874,9 +878,8 @@ __global__ __launch_bounds__(64 * kW, (kMinWaves<kD, kG, kNT, kW>)) void kv_attn
 
 template <int kBits, int kD, int kG, int kNT, bool kShare, int kW>
 void launch_nt(const KvAttnArgs& a, hipStream_t st) {
-  constexpr int kKT = !kShare ? 4 : kD * kBits <= 512 && kD == kG && kW == 4 ? 4 : 2;
   const dim3 grid(static_cast<uint32_t>(static_cast<int64_t>(a.B) * a.Hkv * a.tiles * a.splits));
-  hipLaunchKernelGGL((kv_attn_kernel<kBits, kD, kG, kNT, kShare, kKT, kW>), grid, dim3(64 * kW), 0, st, a);
+  hipLaunchKernelGGL((kv_attn_kernel<kBits, kD, kG, kNT, kShare, kW>), grid, dim3(64 * kW), 0, st, a);
 }
 
 template <int kBits, int kD, int kG>
