@@ -12,11 +12,12 @@
 // sums at the end: where a unit has one workgroup, one group leaves it idle
 // between a barrier and the reads after it.
 //
-// What bounds it: LDS.  Per step of a 256 x 256 tile a unit's waves read 192 KB
-// of fragments and write 64 KB, 2048 clocks at 128 B a clock, as long as the
-// matrix instructions take (128 x 128 a wave would read less, but one wave a
-// SIMD overlapped worse: 1.93 instead of 2.2 POP/s).  8192 x 8192 x 8192:
-// 500 us, 2.2 POP/s; 8192 rows x 4096 x 8192: 314 us, 1.75 POP/s (a prologue
+// What bounds it: matrix instructions and LDS, and how far they overlap.  Per step
+// of a 256 x 256 tile a unit's waves read 192 KB of fragments and write 64 KB,
+// 2048 clocks at 128 B a clock, as long as the matrix instructions take; either
+// is at work half the time (128 x 128 a wave would read less, but one wave a SIMD
+// overlapped worse: 1.93 instead of 2.2 POP/s).  8192 x 8192 x 8192:
+// 500 us, 2.2 POP/s; 8192 rows x 4096 x 8192: 270 us, 2.0 POP/s (a prologue
 // and an epilogue a tile of 32 steps).
 //
 // The 16-byte slots of a row are XOR-swizzled, so publishing and fragment

@@ -29,10 +29,12 @@
 //
 // Few rows (decoding): the four waves of a workgroup have the same rows and
 // take turns at the keys, and workgroups divide long sequences between them.
-// What bounds it is the issue of vector instructions, about 550 for 64 keys of a
-// wave, most of them on the codes (2 MFMA operands' worth for every 8 codes),
-// whatever the number of rows up to 16: 48 sequences of up to 8191 keys, 4 bits,
-// D 128, G 128, are 77 us, 3.8 TB/s of the copy's 5.1.
+// What holds it below the copy's 5.1 TB/s is vector instructions, about 550 for
+// 64 keys of a wave, most of them on the codes (2 MFMA operands' worth for every
+// 8 codes), whatever the number of rows up to 16; they are issued 41% of the time,
+// by 1.6 waves a SIMD on average.  48 sequences of up to 8191 keys, 32 heads on 8,
+// 4 bits, D 128, G 128: 70 to 77 us, 3.8 to 4.1 TB/s, the join of the parts 5 of
+// them.
 //
 // Many rows (prompts): the waves have rows of their own and all need the same
 // fragments, so each makes a quarter of them, in LDS, for all four.  Measured,
@@ -40,9 +42,9 @@
 // every wave on its own, 293 so, 277 with the longest tiles of all heads first
 // (4096 queries on themselves, D 64: 174, 136, 136; D 256: 528, 495, 352).  The
 // rest is the softmax, about 16 vector instructions for 64 scores, next to the
-// products: 37% of the time goes to issuing the former, 19% to the latter, with
-// two waves a SIMD to fill the waits (216 registers).  Four row blocks a wave,
-// one wave a SIMD, took 582 instead of 292.
+// products: the former are issued 41% of the time, the latter run 21% of it, two
+// waves a SIMD fill the waits (216 registers; 1.3 on average, workgroups being of
+// unequal length).  Four row blocks a wave, one wave a SIMD, took 582 instead of 292.
 //
 // Running maxima are renewed only when a score passes the present one by
 // 2^kSlack (probabilities then reach 2^kSlack, which fp16 has room for), and

@@ -12,6 +12,11 @@
 // steps rounded up to bf16 (to bf16 because the exponent range of every input
 // type has to fit): every value then lies within [lo, lo + L * step], so it is
 // at most half a step from the value its code stands for.
+//
+// Memory bounds it where there are many tokens: 16384 of 8 heads of 128 channels,
+// bf16 and 4 bits, 85 MB either way, are written in 22 to 25 us and read in 16 to
+// 19; 64 tokens are a launch, 3 us.  Without the exchanges writing took 21.7,
+// without the parameters' stores (2 bytes of a slot each) 22.8.
 #include <type_traits>
 
 #include "elem.h"
