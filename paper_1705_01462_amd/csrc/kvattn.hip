@@ -109,11 +109,11 @@ struct Plan {
 // 131072 keys and 16 (sequence, key head) pairs: 1.5 a unit 88, 3 70, 6 80, 12
 // 88; 48 sequences of up to 8191: 85, 80, 82, 84), but not below 256 keys, two
 // steps of each of four waves.
-Plan plan(int32_t D, bool wide, int32_t Hq, int32_t Hkv, int64_t B, int64_t max_q, int64_t max_keys, int64_t window) {
+Plan plan(int32_t D, int blocks, bool wide, int32_t Hq, int32_t Hkv, int64_t B, int64_t max_q, int64_t max_keys, int64_t window) {
   Plan p{};
   const int64_t rows = max_q * (Hq / Hkv), cus = ig::device_cus();
   p.share = rows <= 64 || B * Hkv * ceil_div(rows, 128) <= (D == 256 ? cus / 2 : cus);
-  p.nt = rows <= 16 ? 1 : 2;
+  p.nt = rows <= 16 ? 1 : blocks;
   p.tiles = static_cast<int>(ceil_div(rows, 16 * p.nt * (p.share ? 1 : 4)));
   // keys that a tile's rows can see, and its first step's alignment
   const int64_t keys = (window ? std::min(max_keys, window + max_q) : max_keys) + kKvAttnAlign;
@@ -139,13 +139,13 @@ Plan plan(int32_t D, bool wide, int32_t Hq, int32_t Hkv, int64_t B, int64_t max_
 
 size_t kv_attn_ws_bytes(int64_t T, int32_t Hq, int32_t Hkv, int32_t D, int64_t B, int64_t max_q, int64_t max_keys) {
   // of any group size and window
-  const Plan p = plan(D, false, Hq, Hkv, B, max_q, max_keys, 0);
+  const Plan p = plan(D, 2, false, Hq, Hkv, B, max_q, max_keys, 0);
   return p.max_splits == 1 ? 0 : static_cast<size_t>(T) * Hq * p.max_splits * (D + 2) * sizeof(float);
 }
 
 fgq_status launch_kv_attn(KvAttnArgs a, void* ws, hipStream_t st) {
-  const Plan p = plan(a.D, kv_attn_has_wide(a.D, a.G), a.Hq, a.Hkv, a.B, a.max_q, a.max_pages * a.P,
-                      a.window);
+  const Plan p = plan(a.D, kv_attn_blocks(a.D, a.G), kv_attn_has_wide(a.D, a.G), a.Hq, a.Hkv, a.B, a.max_q,
+                      a.max_pages * a.P, a.window);
   a.tiles = p.tiles;
   a.splits = p.splits;
   a.wide = p.wide ? 1 : 0;

@@ -886,19 +886,20 @@ void launch_nt(const KvAttnArgs& a, hipStream_t st) {
 
 template <int kBits, int kD, int kG>
 fgq_status launch_one(const KvAttnArgs& a, int nt, bool share, hipStream_t st) {
+  constexpr int kMost = kv_attn_blocks(kD, kG);
   if (!share) {
-    launch_nt<kBits, kD, kG, 2, false, 4>(a, st);
+    launch_nt<kBits, kD, kG, kMost, false, 4>(a, st);
   } else if (a.wide) {
-    if constexpr (kD < 256 && kD / kG <= 2) {
+    if constexpr (kv_attn_has_wide(kD, kG)) {
       if (nt == 1)
         launch_nt<kBits, kD, kG, 1, true, 8>(a, st);
       else
-        launch_nt<kBits, kD, kG, 2, true, 8>(a, st);
+        launch_nt<kBits, kD, kG, kMost, true, 8>(a, st);
     }
   } else if (nt == 1) {
     launch_nt<kBits, kD, kG, 1, true, 4>(a, st);
   } else {
-    launch_nt<kBits, kD, kG, 2, true, 4>(a, st);
+    launch_nt<kBits, kD, kG, kMost, true, 4>(a, st);
   }
   return last_launch();
 }
