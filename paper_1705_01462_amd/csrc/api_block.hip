@@ -33,9 +33,7 @@ fgq_status check_cache(int64_t num_pages, int32_t Hkv, int32_t D, int32_t P, int
 }
 
 // Whether fgq_linear_i8 quantizes the rows in the product itself.
-bool linear_fused(int64_t M, int64_t K) {
-  return M <= kI8FusedRows && M * (round_up(K, kI8RowStep) + 16) <= kI8FusedBytes;
-}
+bool linear_fused(int64_t M, int64_t K) { return i8_fused(M, round_up(K, kI8RowStep)); }
 
 // Workgroups of the cache's kernels: tokens in 31 bits, heads in 16.
 bool kv_grid_ok(int64_t T, const KvGeom& c) { return T < (1LL << 31) && c.Hkv < (1 << 16); }

@@ -60,9 +60,15 @@ fgq_status launch_i8_few(const i8::I8Args& a, int32_t y_type, hipStream_t st);
 // 16 of them, whose codes fit in LDS.
 fgq_status launch_i8_fused(const void* x, int32_t x_type, int64_t ldx, int64_t K, const i8::I8Args& a, int32_t y_type,
                            hipStream_t st);
-// Measured, us (fused, two launches): K 4096, O 4096, 1 row 8.0, 10.1; 4 rows 8.8,
-// 10.3; 8 rows 10.4, 10.7; 16 rows (K 2048) 8.1, 7.6; K 16384, O 8192, 1 row
-// 31.2, 34.8.
-constexpr int64_t kI8FusedRows = 8, kI8FusedBytes = 64 << 10;
+// When that is done: up to 8 rows (a wave each), and up to 16 short ones.
+// Measured, us (fused, two launches; replayed from a graph, and called one by one,
+// where a launch costs the host as much as the kernel takes): 8 rows of 2048,
+// O 2048 6.5, 6.8 and 8.3, 12.9; of 4000, O 4096 11.5, 10.6 and 11.3, 13.0; 1 row of
+// 4096, O 4096 6.4, 10.1; of 16384, O 8192 31.2, 34.8; 16 rows of 512, O 1024 5.5, 5.2
+// and 8.2, 13.2; of 1024, O 4096 7.0, 6.6 and 8.3, 12.9; of 2048, O 8192 12.6, 9.8 and
+// 12.3, 12.9.
+constexpr bool i8_fused(int64_t M, int64_t row_bytes) {
+  return M * (row_bytes + 16) <= (M <= 8 ? 64 << 10 : M <= 16 ? 17 << 10 : 0);
+}
 
 }  // namespace fgq

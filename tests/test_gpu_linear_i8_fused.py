@@ -1,0 +1,46 @@
+"""GPU: fgq_linear_i8 where the rows are quantized inside the product (no
+workspace) and next to where they no longer are: the same values as
+fgq_quantize_rows followed by fgq_gemm_i8."""
+import numpy as np
+import pytest
+import torch
+
+import block_ref as ref
+
+fgq = pytest.importorskip("paper_1705_01462_amd")
+
+pytestmark = [pytest.mark.gpu,
+              pytest.mark.skipif(not torch.cuda.is_available(), reason="needs a GPU")]
+
+
+@pytest.mark.parametrize("dtype", ref.DTYPES)
+@pytest.mark.parametrize("M,K,fused", [
+    (1, 65408, True), (1, 65537, False), (3, 21000, True), (8, 8064, True), (8, 8200, False), (9, 1, True), (9, 1792, True),
+    (9, 1930, False), (11, 1001, True), (15, 1024, True), (16, 1024, True), (16, 1025, False), (17, 64, False)])
+def test_either_side_of_the_limit(M, K, fused, dtype):
+    r = np.random.default_rng(M * 7 + K)
+    O = 75
+    assert (fgq.fgq_linear_i8_ws_bytes(M, K, O) == 0) == fused
+    x = torch.from_numpy((r.standard_normal((M, K)) * 10.0 ** r.integers(-3, 3, (M, 1))).astype(np.float32))
+    x[M // 2, K // 2] = 0
+    x = x.to(dtype).cuda()
+    w, sw = fgq.fgq_quantize_rows(torch.from_numpy(r.standard_normal((O, K)).astype(np.float32)).cuda())
+    bias = torch.from_numpy(r.standard_normal(O).astype(np.float32)).cuda()
+    q, sx = fgq.fgq_quantize_rows(x)
+    assert torch.equal(fgq.fgq_linear_i8(x, w, sw, bias=bias),
+                       fgq.fgq_gemm_i8(q, sx, K, w, sw, bias=bias, dtype=dtype))
+
+
+@pytest.mark.parametrize("M", [8, 9, 16])
+def test_rows_of_zeros_and_rows_that_are_not_finite(M):
+    K, O = 500, 40
+    r = np.random.default_rng(M)
+    x = torch.from_numpy(r.standard_normal((M, K)).astype(np.float32)).cuda()
+    w, sw = fgq.fgq_quantize_rows(torch.from_numpy(r.standard_normal((O, K)).astype(np.float32)).cuda())
+    want = fgq.fgq_linear_i8(x, w, sw)
+    x[M - 1, 3] = float("inf")
+    x[M - 2] = 0
+    x[0, K - 1] = float("nan")
+    got = fgq.fgq_linear_i8(x, w, sw)
+    assert torch.isnan(got[[0, M - 1]]).all() and not got[M - 2].any()
+    assert torch.equal(got[1:M - 2], want[1:M - 2])
