@@ -1,8 +1,8 @@
-// i8few.hip -- the int8 product at few rows: a workgroup takes 16 channels
+// i8few.hip -- the int8 product at few rows: a workgroup takes 16 kCB channels
 // and 16 kMB rows, its eight waves share the steps of k and meet in LDS.
 //
 // The weights are what such a product has to read.  A wave takes every eighth
-// 128-byte step of k, of 16 channels and of the rows, several steps in flight:
+// 128-byte step of k, of its channels and of the rows, several steps in flight:
 // the bytes in flight, not the instructions, set the rate.  Eight lanes load a
 // row's 128 bytes, and the fragments of the 16x16x64 matrix instruction (lane
 // l: row l % 16, k 16 (l / 16) of 64) are made through LDS of the wave's own.
@@ -33,37 +33,37 @@ constexpr int kAheadFor = kMB <= 2 ? 4 : 3;
 // 16 consecutive rows) touch every bank once.
 __device__ inline int frag_off(int row, int slot) { return row * 128 + 16 * (slot ^ ((row & 7) ^ (row >> 3 & 1))); }
 
-template <int kMB, int kXType, int kType>
+template <int kMB, int kCB, int kXType, int kType>
 __global__ __launch_bounds__(kThreads, 1) void i8_few_kernel(I8Args a, const void* x, int64_t ldx, int64_t K) {
   constexpr bool kFused = kXType >= 0;
   extern __shared__ __attribute__((aligned(16))) unsigned char dyn[];  // fused: codes of the rows
   constexpr int kAhead = kAheadFor<kMB>;
   constexpr int kXRows = kFused ? 0 : 16 * kMB;  // rows of x a wave stages
   // a wave's stage, later its sums
-  __shared__ __attribute__((aligned(16))) unsigned char stage[kWaves][(16 + kXRows) * 128];
-  static_assert((16 + kXRows) * 128 >= kMB * 1024, "");
+  __shared__ __attribute__((aligned(16))) unsigned char stage[kWaves][(16 * kCB + kXRows) * 128];
+  static_assert((16 * kCB + kXRows) * 128 >= kCB * kMB * 1024 && kCB * kMB <= kWaves, "");
   __shared__ uint32_t rmax[kWaves];
   __shared__ float rscale[16];
   const int tid = threadIdx.x, lane = tid % 64;
   const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
   const int g = lane / 16;
-  const int n_ot = (a.O + 15) / 16;
-  const int o0 = 16 * (blockIdx.x % n_ot);
+  const int n_ot = (a.O + 16 * kCB - 1) / (16 * kCB);
+  const int o0 = 16 * kCB * (blockIdx.x % n_ot);
   const int64_t m0 = static_cast<int64_t>(16 * kMB) * (blockIdx.x / n_ot);
   const int rows = static_cast<int>(min(static_cast<int64_t>(16 * kMB), a.M - m0));
   const int64_t pitch = 128LL * a.nk + 16;
 
   // lane l loads slot l % 8 of row l / 8 (+ 8, + 16, ...)
   const int lrow = lane / 8, lslot = lane % 8;
-  const int8_t* wp[2];
+  const int8_t* wp[2 * kCB];
 #pragma unroll
-  for (int j = 0; j < 2; ++j)
+  for (int j = 0; j < 2 * kCB; ++j)
     wp[j] = a.w + min(static_cast<int64_t>(o0 + 8 * j + lrow), static_cast<int64_t>(a.O) - 1) * a.ldw + 16 * lslot;
   const int nw = (a.nk - wave + kWaves - 1) / kWaves;  // this wave's steps: wave, wave + kWaves, ...
-  v4i rw[kAhead][2];
+  v4i rw[kAhead][2 * kCB];
   auto load_w = [&](int u, int i) {
 #pragma unroll
-    for (int j = 0; j < 2; ++j) rw[u][j] = *reinterpret_cast<const v4i*>(wp[j] + 128LL * (wave + kWaves * i));
+    for (int j = 0; j < 2 * kCB; ++j) rw[u][j] = *reinterpret_cast<const v4i*>(wp[j] + 128LL * (wave + kWaves * i));
   };
 #pragma unroll
   for (int u = 0; u < kAhead; ++u)
@@ -152,9 +152,11 @@ __global__ __launch_bounds__(kThreads, 1) void i8_few_kernel(I8Args a, const voi
 #pragma unroll
       for (int j = 0; j < 2 * kMB; ++j) rx[u][j] = *reinterpret_cast<const v4i*>(qp[j] + 128LL * (wave + kWaves * i));
   };
-  v4i acc[kMB];
+  v4i acc[kCB][kMB];
 #pragma unroll
-  for (int b = 0; b < kMB; ++b) acc[b] = v4i{0, 0, 0, 0};
+  for (int c = 0; c < kCB; ++c)
+#pragma unroll
+    for (int b = 0; b < kMB; ++b) acc[c][b] = v4i{0, 0, 0, 0};
 #pragma unroll
   for (int u = 0; u < kAhead; ++u)
     if (u < nw) load_x(u, u);
@@ -166,11 +168,11 @@ __global__ __launch_bounds__(kThreads, 1) void i8_few_kernel(I8Args a, const voi
       if (i < nw) {
         // a wave's LDS accesses are in order: the last step's reads are ahead of these writes
 #pragma unroll
-        for (int j = 0; j < 2; ++j) *reinterpret_cast<v4i*>(mine + frag_off(8 * j + lrow, lslot)) = rw[u][j];
+        for (int j = 0; j < 2 * kCB; ++j) *reinterpret_cast<v4i*>(mine + frag_off(8 * j + lrow, lslot)) = rw[u][j];
         if constexpr (!kFused)
 #pragma unroll
           for (int j = 0; j < 2 * kMB; ++j)
-            *reinterpret_cast<v4i*>(mine + 2048 + frag_off(8 * j + lrow, lslot)) = rx[u][j];
+            *reinterpret_cast<v4i*>(mine + 2048 * kCB + frag_off(8 * j + lrow, lslot)) = rx[u][j];
         if (i + kAhead < nw) {
           load_w(u, i + kAhead);
           load_x(u, i + kAhead);
@@ -178,15 +180,20 @@ __global__ __launch_bounds__(kThreads, 1) void i8_few_kernel(I8Args a, const voi
         wave_fence();
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const v4i wf = *reinterpret_cast<const v4i*>(mine + frag_off(lane % 16, 4 * h + g));
+          v4i wf[kCB];
+#pragma unroll
+          for (int c = 0; c < kCB; ++c)
+            wf[c] = *reinterpret_cast<const v4i*>(mine + frag_off(16 * c + lane % 16, 4 * h + g));
 #pragma unroll
           for (int b = 0; b < kMB; ++b) {
             v4i xf;
             if constexpr (kFused)
               xf = *reinterpret_cast<const v4i*>(lp + 128LL * (wave + kWaves * i) + 64 * h);
             else
-              xf = *reinterpret_cast<const v4i*>(mine + 2048 + frag_off(16 * b + lane % 16, 4 * h + g));
-            acc[b] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wf, xf, acc[b], 0, 0, 0);
+              xf = *reinterpret_cast<const v4i*>(mine + 2048 * kCB + frag_off(16 * b + lane % 16, 4 * h + g));
+#pragma unroll
+            for (int c = 0; c < kCB; ++c)
+              acc[c][b] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wf[c], xf, acc[c][b], 0, 0, 0);
           }
         }
         wave_fence();
@@ -195,31 +202,34 @@ __global__ __launch_bounds__(kThreads, 1) void i8_few_kernel(I8Args a, const voi
   }
 
 #pragma unroll
-  for (int b = 0; b < kMB; ++b) reinterpret_cast<v4i*>(mine)[64 * b + lane] = acc[b];
+  for (int c = 0; c < kCB; ++c)
+#pragma unroll
+    for (int b = 0; b < kMB; ++b) reinterpret_cast<v4i*>(mine)[64 * (kMB * c + b) + lane] = acc[c][b];
   __syncthreads();
-  if (wave < kMB) {
+  if (wave < kCB * kMB) {
+    const int ot = o0 + 16 * (wave / kMB), b = wave % kMB;
     v4i S = reinterpret_cast<const v4i*>(stage[0])[64 * wave + lane];
 #pragma unroll
     for (int w = 1; w < kWaves; ++w) S += reinterpret_cast<const v4i*>(stage[w])[64 * wave + lane];
-    const int64_t m = m0 + 16 * wave + lane % 16;
-    if (16 * wave + lane % 16 < rows) {
+    const int64_t m = m0 + 16 * b + lane % 16;
+    if (16 * b + lane % 16 < rows) {
       const float sx = kFused ? scale : a.sx[m];
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
-        const int o = o0 + 4 * g + c;
+        const int o = ot + 4 * g + c;
         if (o < a.O) put_y<kType>(a, m, o, scaled(S[c], sx, a.sw[o], a.bias ? a.bias[o] : 0.0f));
       }
     }
   }
 }
 
-template <int kMB, int kXType, int kType>
+template <int kMB, int kCB, int kXType, int kType>
 fgq_status launch(const I8Args& a, const void* x, int64_t ldx, int64_t K, hipStream_t st) {
-  const int64_t wgs = ceil_div(a.O, 16) * ceil_div(a.M, 16 * kMB);
+  const int64_t wgs = ceil_div(a.O, 16 * kCB) * ceil_div(a.M, 16 * kMB);
   if (wgs >= (1LL << 31)) return FGQ_ERR_UNSUPPORTED;
   const uint32_t dyn = kXType < 0 ? 0 : static_cast<uint32_t>(a.M * (128 * a.nk + 16));
-  hipLaunchKernelGGL((i8_few_kernel<kMB, kXType, kType>), dim3(static_cast<uint32_t>(wgs)), dim3(kThreads), dyn, st, a,
-                     x, ldx, K);
+  hipLaunchKernelGGL((i8_few_kernel<kMB, kCB, kXType, kType>), dim3(static_cast<uint32_t>(wgs)), dim3(kThreads), dyn,
+                     st, a, x, ldx, K);
   return last_launch();
 }
 
@@ -228,10 +238,19 @@ fgq_status launch(const I8Args& a, const void* x, int64_t ldx, int64_t K, hipStr
 fgq_status launch_i8_few(const I8Args& a, int32_t y_type, hipStream_t st) {
   return with_type(y_type, [&](auto t) {
     constexpr int kType = decltype(t)::value;
-    if (a.M <= 16) return launch<1, -1, kType>(a, nullptr, 0, 0, st);
-    if (a.M <= 32) return launch<2, -1, kType>(a, nullptr, 0, 0, st);
-    if (a.M <= 48) return launch<3, -1, kType>(a, nullptr, 0, 0, st);
-    return launch<4, -1, kType>(a, nullptr, 0, 0, st);
+    if (a.M <= 16) return launch<1, 1, -1, kType>(a, nullptr, 0, 0, st);
+    if (a.M <= 32) return launch<2, 1, -1, kType>(a, nullptr, 0, 0, st);
+    // 32 channels a workgroup where that still is one a unit (us, 16 and 32: 48 rows
+    // of 16384, 8192 channels 45.4, 36.7; of 4096, 11008 channels 22.4, 21.9; 64 rows
+    // 52.4, 39.7 and 28.4, 24.8; but 20 of 4096, 11008 channels 17.7, 18.6, and 48 of
+    // 9216, 4096 channels, half the units, 16.0, 17.9): the rows, read by every
+    // workgroup, are by then more bytes than the weights.
+    if (ceil_div(a.O, 32) >= ig::device_cus()) {
+      if (a.M <= 48) return launch<3, 2, -1, kType>(a, nullptr, 0, 0, st);
+      return launch<4, 2, -1, kType>(a, nullptr, 0, 0, st);
+    }
+    if (a.M <= 48) return launch<3, 1, -1, kType>(a, nullptr, 0, 0, st);
+    return launch<4, 1, -1, kType>(a, nullptr, 0, 0, st);
   });
 }
 
@@ -239,7 +258,7 @@ fgq_status launch_i8_fused(const void* x, int32_t x_type, int64_t ldx, int64_t K
                            hipStream_t st) {
   return with_type(x_type, [&](auto xt) {
     return with_type(y_type, [&](auto t) {
-      return launch<1, decltype(xt)::value, decltype(t)::value>(a, x, ldx, K, st);
+      return launch<1, 1, decltype(xt)::value, decltype(t)::value>(a, x, ldx, K, st);
     });
   });
 }

@@ -20,10 +20,11 @@ def run_cases(fgq, torch):
             out[f"{name}_{i}"] = (v.view(torch.int16) if v.dtype is torch.bfloat16 else v).cpu().numpy()
 
     types = [torch.float32, torch.float16, torch.bfloat16]
-    # every tile of the products, and the few-row forms with 1 to 4 row blocks, ragged
+    # every tile of the products, and the few-row forms with 1 to 4 row blocks (and two channel blocks), ragged
     for i, (M, K, O) in enumerate([(1, 333, 37), (7, 4100, 33), (13, 700, 65), (30, 1001, 77), (48, 512, 100),
                                    (61, 2049, 16), (70, 300, 1000), (300, 260, 2000), (700, 130, 1900),
-                                   (1030, 200, 2100), (900, 3300, 700), (2100, 513, 3000), (3000, 300, 5000)]):
+                                   (1030, 200, 2100), (900, 3300, 700), (2100, 513, 3000), (3000, 300, 5000),
+                                   (40, 260, 8200), (60, 1300, 9001)]):
         x, w, b = t(r.standard_normal((M, K)), types[i % 3]), t(r.standard_normal((O, K))), t(r.standard_normal(O))
         wq, sw = fgq.fgq_quantize_rows(w)
         keep(f"linear{i}", fgq.fgq_linear_i8(x, wq, sw, bias=b, dtype=types[(i + 1) % 3]))

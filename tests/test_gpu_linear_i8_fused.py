@@ -44,3 +44,18 @@ def test_rows_of_zeros_and_rows_that_are_not_finite(M):
     got = fgq.fgq_linear_i8(x, w, sw)
     assert torch.isnan(got[[0, M - 1]]).all() and not got[M - 2].any()
     assert torch.equal(got[1:M - 2], want[1:M - 2])
+
+
+@pytest.mark.parametrize("O", [8192, 8177, 8209, 9000])
+@pytest.mark.parametrize("M", [33, 48, 49, 64])
+def test_few_rows_of_many_channels(M, O):
+    """Wide workgroups, whose channels end anywhere; sums compared exactly."""
+    K = 700
+    r = np.random.default_rng(M + O)
+    q = torch.zeros((M, fgq.fgq_i8_row_bytes(K)), dtype=torch.int8)
+    w = torch.zeros((O, fgq.fgq_i8_row_bytes(K)), dtype=torch.int8)
+    q[:, :K] = torch.from_numpy(r.integers(-127, 128, (M, K)).astype(np.int8))
+    w[:, :K] = torch.from_numpy(r.integers(-127, 128, (O, K)).astype(np.int8))
+    one = lambda n: torch.ones(n, dtype=torch.float32, device="cuda")
+    y = fgq.fgq_gemm_i8(q.cuda(), one(M), K, w.cuda(), one(O))
+    assert torch.equal(y.cpu().double(), q.double() @ w.double().T)
